@@ -71,7 +71,8 @@ typedef enum {
     LLLA_ERR_LAUNCH = 8       /* the HIP runtime refused a launch */
 } llla_status;
 
-typedef enum { LLLA_F32 = 0, LLLA_BF16 = 1 } llla_dtype;
+/* LLLA_I8 and LLLA_E4M3 are types of the rows of an llla_cache (below); every other argument takes the first two. */
+typedef enum { LLLA_F32 = 0, LLLA_BF16 = 1, LLLA_I8 = 2, LLLA_E4M3 = 3 } llla_dtype;
 
 /* Element strides of a [batch, head, seq, d] tensor; the d stride is 1 by contract.
  * Each must be a multiple of 4 (f32) or 8 (bf16) elements so that rows stay 16-byte aligned. */
@@ -242,6 +243,100 @@ llla_status llla_decode_static(const void *q, const void *Kc, const void *Vc, vo
                                llla_strides sk, llla_strides sv, const int32_t *seqlens,
                                int B, int H, int L_max, int d, llla_dtype in, llla_dtype out,
                                float lambda, float scale, void *stream);
+
+/*
+ * The cache of a serving loop, and what is done to it between two tokens: rows are stored, attended to, weighed and given up.
+ *
+ * llla_cache -- keys and values of B sequences and H cache heads, slots 0 .. L_max - 1.
+ *   K, V         : device, [B, H, L_max, d] in `type`, strides sk / sv (8-bit types: multiples of 16 elements; below 2^27)
+ *   k_exp, v_exp : device int8 [B, H, ceil(L_max / LLLA_CACHE_BLOCK)] contiguous; 8-bit types only, ignored otherwise
+ *   scores       : device float [B, H, L_max] contiguous: the weight a row has gathered; NULL where a call does not need it
+ *   pos          : device int32 [B, H, L_max] contiguous: the position in its sequence that a row stands for; NULL: its slot
+ * 8-bit rows are codes c, int8 in [-127, 127] or e4m3 (4 exponent bits, 3 of mantissa, largest 448, no infinities), and stand for
+ * c * 2^e, e = k_exp / v_exp of the block of LLLA_CACHE_BLOCK slots that the row is in.  Codes times a power of two are exact in
+ * bf16 and f16, so a call over such a cache is the call over rows of numbers.  e = -128 marks a block that was given a value that is not finite:
+ * all its rows read as NaN, until the block is filled anew from its first slot.
+ * The exponent of a block is the smallest e >= -120 with max |x| <= 127 * 2^e (int8) or 448 * 2^e (e4m3), rows are rounded to the nearest code,
+ * ties to even.  It only grows while rows come in, in which case the rows that are there are rounded again: in e4m3 exactly, but for subnormal codes.
+ * Lengths (seqlens: device int32 [B]) are taken as 0 .. L_max; slots at and behind a sequence's length hold nothing, and are written by
+ * llla_cache_append alone.  Calls that write a cache and others that use it are ordered by the caller, on one stream or by events.
+ */
+#define LLLA_CACHE_BLOCK 64
+
+typedef struct {
+    void *K, *V;
+    llla_strides sk, sv;
+    int8_t *k_exp, *v_exp;
+    float *scores;
+    int32_t *pos;
+    int B, H, L_max, d;
+    llla_dtype type;
+} llla_cache;
+
+/*
+ * llla_cache_append -- stores the next n rows of every sequence: k[b, h, i], v[b, h, i] go to slot seqlens[b] + i.
+ *   k, v      : device, [B, H, n, d] in dtype `in` (LLLA_F32 or LLLA_BF16), strides sk / sv, not overlapping the cache
+ *   seqlens   : rows that are there; NULL = none.  The caller adds what was stored
+ *   new_lens  : device int32 [B], rows that sequence b brings, at most n (the others of its n are not read); NULL = n
+ *   first_pos : device int32 [B], position of a sequence's first new row (the next ones follow); NULL = its slot.  For cache->pos
+ * cache->scores, if any, becomes 0 at the new rows.  Rows that would go beyond L_max are not stored.  Rows of 32 or 16 bits are converted
+ * to the cache's type, to nearest even.
+ */
+llla_status llla_cache_append(const llla_cache *cache, const void *k, const void *v, llla_strides sk, llla_strides sv, int n,
+                              llla_dtype in, const int32_t *seqlens, const int32_t *new_lens, const int32_t *first_pos,
+                              void *stream);
+
+/*
+ * llla_decode_q8 -- llla_decode over an 8-bit cache: one new query per (sequence, query head) against the rows of its cache head,
+ * query head h reading cache head h / (H / cache->H).
+ *   q       : device, [B, H, d] contiguous, dtype `in` (LLLA_F32 or LLLA_BF16);  H a multiple of cache->H
+ *   o       : device, [B, H, d] contiguous, dtype `out`
+ *   seqlens : valid lengths, or NULL = all L_max; the result of an empty sequence is zero
+ * fp32 arithmetic for every type: sequences of at most 64 keys in key space in fp64, longer ones on 16-bit matrix instructions that take
+ * the codes as they are and the weighted keys in two terms of 11 bits.  There is no range of values to keep to; rows of a block whose exponent is
+ * more than 15 (int8) or 22 (e4m3) below the largest of their head's lose low bits, at most 2^-23 of the largest row.
+ * Workspace: llla_decode_q8_workspace_bytes, or NULL (or less): one workgroup per head, slow for long caches of few heads.
+ */
+size_t llla_decode_q8_workspace_bytes(const llla_cache *cache, int H);
+
+llla_status llla_decode_q8(const void *q, const llla_cache *cache, void *o, const int32_t *seqlens, int H,
+                           llla_dtype in, llla_dtype out, float lambda, float scale,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * llla_cache_scores -- adds to cache->scores the share of every query's kernel weight that a row has:
+ *     scores[b, h, j] += sum over the queries i of the H / cache->H query heads of h of  w_ij / omega_i
+ * (w, omega as at the top of this file).  What a row takes part in, omega, mu and Sigma, it does in proportion to w_ij: a row that gathers little can be
+ * given up without changing a query's system.  (The output weights s_ij of Eq. (lla) can be negative, and are zero for rows that still shape it.)
+ *   Q       : device, [B, H, nq, d] in dtype `in`, strides sq: the queries of the last nq rows, that is query i stands at slot
+ *             seqlens[b] - nq + i and sees the slots up to its own (nq = 1: a decode step); one in front of slot 0 sees nothing and adds nothing
+ *   cache   : K of any type, rows of 32 and 16 bits in the type of the queries; V is not read
+ *   seqlens : valid lengths, or NULL = all L_max
+ * Workspace: llla_cache_scores_workspace_bytes.
+ */
+size_t llla_cache_scores_workspace_bytes(const llla_cache *cache, int H, int nq, llla_dtype in);
+
+llla_status llla_cache_scores(const void *Q, const llla_cache *cache, llla_strides sq, const int32_t *seqlens, int H, int nq,
+                              llla_dtype in, float scale, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * llla_cache_evict -- keeps `keep` rows of every (sequence, head) and gives up the others: the first `sinks` and last `recent` positions
+ * (pos < sinks, pos > newest - recent, newest the largest of the head) before all others, then those of larger score, then those of lower
+ * slot.  A score that is NaN is the smallest.  Sequences of at most `keep` rows keep all.
+ *   into  : NULL: in place.  Rows kept in slots from `keep` on move to the slots below of rows given up, the first to the first, and so on:
+ *           attention does not depend on the order of the rows, so no other row moves.  pos tells what a row stands for afterwards.
+ *           Another cache of the same B, H, d and type and L_max >= keep, which shares no memory with `cache`: rows are copied there, in the
+ *           order of their slots; `cache` stays as it is.
+ *   lens  : device int32 [B], the lengths afterwards, min(length, keep); not the array `seqlens`
+ *   index : device int32 [B, H, keep] contiguous or NULL: the slot that row j was in before; entries from the new length on are not written
+ * scores (required) and pos, where both caches have them, move with the rows.  In an 8-bit cache rows that come into a block are written in its
+ * exponent, which grows as far as they need it.
+ * sinks, recent >= 0, sinks + recent <= keep.  Workspace: llla_cache_evict_workspace_bytes.
+ */
+size_t llla_cache_evict_workspace_bytes(const llla_cache *cache, int keep);
+
+llla_status llla_cache_evict(const llla_cache *cache, const llla_cache *into, const int32_t *seqlens, int keep, int sinks,
+                             int recent, int32_t *lens, int32_t *index, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char *llla_status_string(llla_status status);

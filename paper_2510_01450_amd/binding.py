@@ -78,6 +78,8 @@ def _declare(L, measure: bool):
     L.llla_decode_path.restype = i32
     L.llla_decode_static.argtypes = dec + [vp]
     L.llla_decode_static.restype = i32
+    from . import cache
+    cache.declare(L)
     L.llla_status_string.argtypes = [i32]
     L.llla_status_string.restype = ctypes.c_char_p
     L.llla_version.restype = ctypes.c_char_p

@@ -545,26 +545,11 @@ __device__ __forceinline__ void finish_workgroup(Lds &lds, f32x4 (&acc)[DecShape
 // thread and a compute unit takes 1 us for it however many are requested together.  Eight (at d = 64) take more registers than two workgroups on
 // a compute unit have: 512 heads x 8192 170 instead of 164 us.  us of a call, eight at a time and so: d = 128, 8 heads x 1000 keys 48.7 / 44.1,
 // 16 x 4096 69.5 / 63.9; d = 64, 16 x 4096 28.4 / 26.1; fp32, 16 x 4096 40.0 / 35.6; d = 16, fp32, 64 heads of 512 .. 4096 24.9 / 20.5.
-// DUAL: a call whose sequences of at most 64 keys are served in key space has one more workgroup per head for that, in the same
-// launch; which of the two writes the head follows from its length.
-template <int D, typename TI, bool PERM, bool DUAL = false>
-__global__ __launch_bounds__(DEC_NT, D == 128 ? 1 : 2) void decode_merge_kernel(DecSplit split, HeadOut out, const float *__restrict__ parts,
-                                                                 dual::DualArgs da = {}, int heads = 0)
+template <int D, typename TI, bool PERM>
+__device__ __forceinline__ void merge_head(HeadLds<D, 1, 1> &lds, const DecSplit &split, const HeadOut &out, const float *__restrict__ parts, int bh)
 {
     using S = DecShape<D>;
-    using Dual = dual::DualShared<D, DUAL_MAX_KEYS>;
-    constexpr size_t LDS_B = sizeof(HeadLds<D, 1, 1>) > sizeof(Dual) || !DUAL ? sizeof(HeadLds<D, 1, 1>) : sizeof(Dual);
-    __shared__ __align__(16) unsigned char raw[LDS_B];
-    if constexpr (DUAL) {
-        if ((int)blockIdx.x >= heads) {
-            if (out.out_bf16) dual::dual_decode_head<D, TI, bf16_t>(*reinterpret_cast<Dual *>(raw), da, split.seqlens, blockIdx.x - heads);
-            else dual::dual_decode_head<D, TI, float>(*reinterpret_cast<Dual *>(raw), da, split.seqlens, blockIdx.x - heads);
-            return;
-        }
-        if (seq_len(split, blockIdx.x / split.H) <= DUAL_MAX_KEYS) return;
-    }
-    HeadLds<D, 1, 1> &lds = *reinterpret_cast<HeadLds<D, 1, 1> *>(raw);
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, bh = blockIdx.x;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64;
     const QueryPart<D> q = load_query<D, TI, PERM>(out, bh, lane);
     const DecRecords rec = dec_records(split, bh);
     const int np = rec.count;
@@ -625,6 +610,26 @@ __global__ __launch_bounds__(DEC_NT, D == 128 ? 1 : 2) void decode_merge_kernel(
     if (tid == 0) lds.om[0] = om;
     __syncthreads();
     solve_head<D, TI, PERM>(lds, out, q, bh, wave, lane);
+}
+
+// DUAL: a call whose sequences of at most 64 keys are served in key space has one more workgroup per head for that, in the same
+// launch; which of the two writes the head follows from its length.
+template <int D, typename TI, bool PERM, bool DUAL = false>
+__global__ __launch_bounds__(DEC_NT, D == 128 ? 1 : 2) void decode_merge_kernel(DecSplit split, HeadOut out, const float *__restrict__ parts,
+                                                                 dual::DualArgs da = {}, int heads = 0)
+{
+    using Dual = dual::DualShared<D, DUAL_MAX_KEYS>;
+    constexpr size_t LDS_B = sizeof(HeadLds<D, 1, 1>) > sizeof(Dual) || !DUAL ? sizeof(HeadLds<D, 1, 1>) : sizeof(Dual);
+    __shared__ __align__(16) unsigned char raw[LDS_B];
+    if constexpr (DUAL) {
+        if ((int)blockIdx.x >= heads) {
+            if (out.out_bf16) dual::dual_decode_head<D, TI, bf16_t>(*reinterpret_cast<Dual *>(raw), da, split.seqlens, blockIdx.x - heads);
+            else dual::dual_decode_head<D, TI, float>(*reinterpret_cast<Dual *>(raw), da, split.seqlens, blockIdx.x - heads);
+            return;
+        }
+        if (seq_len(split, blockIdx.x / split.H) <= DUAL_MAX_KEYS) return;
+    }
+    merge_head<D, TI, PERM>(*reinterpret_cast<HeadLds<D, 1, 1> *>(raw), split, out, parts, blockIdx.x);
 }
 
 }  // namespace mfma

@@ -78,9 +78,10 @@ struct DualArgs {
     int nrows;                                     // rows [0, nrows) are served here
 };
 
-// Row i of (batch, head) bh, which sees m <= MK keys: output row O, statistics rho, delta (either may be NULL)
-template <int D, typename TI, typename TO, class Shared>
-__device__ __forceinline__ void dual_row(Shared &sm, const TI *qrow, const TI *Kh, const TI *Vh, int64_t kseq, int64_t vseq,
+// Row i of (batch, head) bh, which sees m <= MK keys: output row O, statistics rho, delta (either may be NULL).  Rows: where the keys and values
+// begin, a pointer to numbers or anything else that ld_f32 reads and an offset moves.
+template <int D, typename TI, typename TO, class Shared, class Rows>
+__device__ __forceinline__ void dual_row(Shared &sm, const TI *qrow, Rows Kh, Rows Vh, int64_t kseq, int64_t vseq,
                                          int m, double lam, float scale, TO *orow, float *rho, float *delta)
 {
     constexpr int MK = Shared::MK, d = D;

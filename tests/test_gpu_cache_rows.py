@@ -1,0 +1,303 @@
+"""Rows that come into a cache (llla_cache_append) and rows that stay in it (llla_cache_evict): every tensor of the cache bit by bit against a plain
+implementation."""
+import pytest
+import torch
+
+import cache_reference as ref
+import paper_2510_01450_amd as llla
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+I8, E4M3, BF16, F32 = torch.int8, torch.float8_e4m3fn, torch.bfloat16, torch.float32
+
+
+def _gen(seed):
+    return torch.Generator(device="cpu").manual_seed(seed)
+
+
+def _rows(gen, shape, spread=1.0):
+    x = torch.randn(shape, generator=gen, dtype=torch.float32)
+    return x * torch.exp(spread * torch.randn(shape[:-1] + (1,), generator=gen))
+
+
+def _padded(x, extra):
+    """The same numbers in a tensor whose rows, heads and sequences lie `extra` elements further apart."""
+    B, H, n, d = x.shape
+    big = torch.zeros((B, H + 1, n + 1, d + extra), dtype=x.dtype, device=x.device) if x.dtype != E4M3 else \
+        torch.zeros((B, H + 1, n + 1, d + extra), dtype=torch.uint8, device=x.device).view(E4M3)
+    view = big[:, :H, :n, :d]
+    ref.bits(view).copy_(ref.bits(x))
+    return view
+
+
+def _cache(gen, B, H, L, d, dtype, lens, pos="slots", spread=1.0):
+    """A cache with rows in its first lens[b] slots, garbage behind them."""
+    cache = llla.cache_alloc(B, H, L, d, dtype, DEV, scores=True, pos=pos is not None)
+    for t in (cache.K, cache.V):
+        if dtype in ref.CODES:
+            ref.bits(t).copy_(torch.randint(0, 126, t.shape, generator=gen).to(DEV))
+        else:
+            t.copy_(torch.randn(t.shape, generator=gen).to(DEV))
+    if dtype in ref.CODES:
+        for e in (cache.k_exp, cache.v_exp):
+            e.copy_(torch.randint(-9, 4, e.shape, generator=gen).to(DEV))
+    cache.scores.copy_(torch.exp(2 * torch.randn(cache.scores.shape, generator=gen)).to(DEV))
+    if pos == "mixed":
+        cache.pos.copy_(torch.stack([torch.randperm(L, generator=gen) for _ in range(B * H)]).view(B, H, L).to(DEV))
+    elif pos is not None:
+        cache.pos.copy_(torch.arange(L).expand(B, H, L).to(DEV))
+    n = max(lens)
+    if n:
+        k, v = _rows(gen, (B, H, n, d), spread).to(DEV), _rows(gen, (B, H, n, d), spread).to(DEV)
+        keep = (cache.scores.clone(), None if cache.pos is None else cache.pos.clone())
+        llla.llla_cache_append(cache, k, v, new_lens=torch.tensor(lens, dtype=torch.int32, device=DEV))
+        cache.scores.copy_(keep[0])
+        if pos == "mixed":
+            cache.pos.copy_(keep[1])
+    return cache
+
+
+def _same(cache, host, what):
+    for name, t in zip(("K", "V", "ke", "ve", "scores", "pos"), cache):
+        if t is None:
+            continue
+        got, want = ref.bits(t).cpu(), ref.bits(getattr(host, name))
+        if got.dtype in (torch.float32, torch.bfloat16):
+            ok = torch.equal(torch.nan_to_num(got.float(), nan=12345.0), torch.nan_to_num(want.float(), nan=12345.0))
+        else:
+            ok = torch.equal(got, want)
+        if not ok:
+            bad = torch.nonzero(got != want)
+            raise AssertionError("%s: %s differs at %d places, first %s: %s instead of %s" % (
+                what, name, len(bad), bad[0].tolist(), got[tuple(bad[0])].item(), want[tuple(bad[0])].item()))
+
+
+def _append(cache, k, v, lens, counts=None, first=None, **kw):
+    i32 = lambda x: None if x is None else torch.tensor(x, dtype=torch.int32, device=DEV)
+    host = ref.Host(cache)
+    llla.llla_cache_append(cache, k, v, seqlens=i32(lens), new_lens=i32(counts), first_pos=i32(first), **kw)
+    torch.cuda.synchronize()
+    ref.append(host, k.cpu(), v.cpu(), lens or [0] * host.B, counts or [k.shape[2]] * host.B, first)
+    return host
+
+
+@pytest.mark.parametrize("dtype", [I8, E4M3, BF16, F32])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+def test_append_at_every_kind_of_place(dtype, d):
+    """Lengths at, before and behind the border of a block, none, all; counts of none to more than a block; rows beyond the capacity."""
+    lens, counts = [0, 1, 63, 64, 65, 150, 200, 130], [7, 0, 1, 64, 65, 51, 3, 129]
+    gen = _gen(d)
+    for n, inp in ((129, F32), (129, BF16)):
+        cache = _cache(gen, 8, 2, 200, d, dtype, lens)
+        k, v = _rows(gen, (8, 2, n, d)).to(inp).to(DEV), _rows(gen, (8, 2, n, d)).to(inp).to(DEV)
+        host = _append(cache, k, v, lens, counts, [5, 0, 100, 64, 7, 150, 200, 9])
+        _same(cache, host, "append %s d=%d %s" % (dtype, d, inp))
+
+
+@pytest.mark.parametrize("dtype", [I8, E4M3])
+@pytest.mark.parametrize("n", [1, 2, 40])
+def test_rows_that_outgrow_their_block(dtype, n):
+    """Every later row is larger: the rows that are there are rounded again, each time."""
+    gen = _gen(n)
+    cache = llla.cache_alloc(2, 3, 130, 64, dtype, DEV)
+    lens = [0, 60]
+    llla.llla_cache_append(cache, *(_rows(gen, (2, 3, 60, 64)).to(DEV) for _ in range(2)), new_lens=torch.tensor([0, 60], dtype=torch.int32, device=DEV))
+    for step in range(4):
+        k, v = (_rows(gen, (2, 3, n, 64)).to(DEV) * 5.0 ** step for _ in range(2))
+        host = _append(cache, k, v, lens)
+        _same(cache, host, "step %d" % step)
+        lens = [min(x + n, 130) for x in lens]
+
+
+@pytest.mark.parametrize("dtype", [I8, E4M3])
+def test_borders_of_the_format(dtype):
+    """Largest values that are exactly a power of two, a code's largest times one, or the next number above; ties; subnormal, zero and huge rows."""
+    top = ref.LARGEST[dtype]
+    d = 16
+    rows = []
+    for e in (-130, -126, -121, -120, -119, -60, -1, 0, 1, 60, 100, 119):
+        for m in (1.0, top / 512, 127 / 128, 0.875, float(torch.nextafter(torch.tensor(top / 512), torch.tensor(2.0)))):
+            rows.append(torch.full((d,), m, dtype=torch.float64) * 2.0 ** e * torch.linspace(-1, 1, d, dtype=torch.float64))
+    rows.append(torch.zeros(d, dtype=torch.float64))
+    rows.append(torch.full((d,), 1e-44, dtype=torch.float64))
+    rows.append(torch.full((d,), 3.4028234e38, dtype=torch.float64))
+    rows.append(torch.arange(d, dtype=torch.float64) / 2 + 120 - d / 2)              # ties of int8
+    x = torch.stack(rows).float()
+    k = x[None, None].expand(1, 1, -1, -1).contiguous()
+    B = k.shape[2]                                                     # a row alone in its block
+    k = k.view(B, 1, 1, d).to(DEV)
+    cache = llla.cache_alloc(B, 1, 64, d, dtype, DEV)
+    host = _append(cache, k, -k, [0] * B)
+    _same(cache, host, "borders")
+
+
+def test_every_e4m3_tie_and_neighbour():
+    """All midpoints between neighbouring e4m3 numbers, and the fp32 numbers beside them."""
+    codes = torch.arange(0, 127, dtype=torch.uint8).view(E4M3).double()
+    mid = ((codes[1:] + codes[:-1]) / 2).float()
+    x = torch.cat([mid, torch.nextafter(mid, torch.tensor(0.0)), torch.nextafter(mid, torch.tensor(1e9))])
+    x = torch.cat([x, -x])
+    x = torch.nn.functional.pad(x, (0, -x.numel() % 15)).view(-1, 15)
+    x = torch.cat([x, torch.full((x.shape[0], 1), 448.0)], 1)                          # exponent 0
+    k = x[None, None, :64].to(DEV)
+    cache = llla.cache_alloc(1, 1, 64, 16, E4M3, DEV)
+    host = _append(cache, k, k, [0])
+    assert int(cache.k_exp[0, 0, 0]) == 0
+    _same(cache, host, "ties")
+
+
+@pytest.mark.parametrize("dtype", [I8, E4M3])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_rows_that_are_not_finite(dtype, bad):
+    """Such a row marks its block, of its tensor alone; a later row does not mend it, filling the block anew does."""
+    gen = _gen(3)
+    cache = _cache(gen, 2, 2, 192, 32, dtype, [10, 70])
+    k, v = _rows(gen, (2, 2, 60, 32)).to(DEV), _rows(gen, (2, 2, 60, 32)).to(DEV)
+    k[0, 1, 2, 5] = bad
+    host = _append(cache, k, v, [10, 70])
+    _same(cache, host, "bad")
+    assert int(cache.k_exp[0, 1, 0]) == -128 and int(cache.v_exp[0, 1, 0]) != -128 and int(cache.k_exp[0, 1, 1]) != -128
+    assert int((cache.k_exp == -128).sum()) == 1
+    host = _append(cache, v[:, :, :1], v[:, :, :1], [20, 130])
+    _same(cache, host, "after")
+    host = _append(cache, v[:, :, :30], v[:, :, :30], [0, 0])
+    _same(cache, host, "anew")
+    assert int(cache.k_exp[0, 1, 0]) != -128
+
+
+@pytest.mark.parametrize("dtype", [I8, E4M3, BF16])
+def test_append_with_other_strides(dtype):
+    """Caches and rows that are parts of larger tensors, and rows laid out token by token ([B, n, H, d] in memory)."""
+    gen = _gen(8)
+    c = _cache(gen, 2, 3, 150, 64, dtype, [20, 64])
+    cache = c._replace(K=_padded(c.K, 16), V=_padded(c.V, 32))
+    k = _rows(gen, (2, 70, 3, 64)).to(BF16).to(DEV).transpose(1, 2)
+    v = _padded(_rows(gen, (2, 3, 70, 64)).to(BF16).to(DEV), 8)
+    around = ref.bits(cache.K._base if cache.K._base is not None else cache.K).clone()
+    host = _append(cache, k, v, [20, 64])
+    _same(cache, host, "strides")
+    whole = ref.bits(cache.K._base).view(around.shape) if cache.K._base is not None else None
+    if whole is not None and whole.dim() == 4 and whole.shape[-1] == 80:
+        assert torch.equal(whole[..., 64:], around[..., 64:]) and torch.equal(whole[:, 3:], around[:, 3:])
+
+
+def _evict(cache, lens, keep, sinks=0, recent=0, into=None, **kw):
+    host, hinto = ref.Host(cache), None if into is None else ref.Host(into)
+    index = torch.full((host.B, host.H, keep), -7, dtype=torch.int32, device=DEV)
+    seq = None if lens is None else torch.tensor(lens, dtype=torch.int32, device=DEV)
+    got = llla.llla_cache_evict(cache, keep, seqlens=seq, sinks=sinks, recent=recent, into=into, index=index, **kw)
+    torch.cuda.synchronize()
+    want, where = ref.evict(host, hinto, lens or [host.L] * host.B, keep, sinks, recent)
+    assert got.cpu().tolist() == want
+    for b in range(host.B):
+        for h in range(host.H):
+            assert index[b, h].cpu().tolist() == where[b][h] + [-7] * (keep - want[b]), (b, h)
+    _same(cache, host, "evict")
+    if into is not None:
+        _same(into, hinto, "evict into")
+
+
+@pytest.mark.parametrize("dtype,d", [(I8, 64), (E4M3, 64), (I8, 16), (E4M3, 32), (I8, 128), (BF16, 64), (BF16, 16), (F32, 32), (F32, 128), (BF16, 128), (F32, 64)])
+@pytest.mark.parametrize("into", [False, True])
+def test_evict_lengths_and_budgets(dtype, d, into):
+    """Budgets at and around the border of a block, one row, all but one; lengths of none, one, the budget, beyond it."""
+    L = 330
+    gen = _gen(d + into)
+    for keep, sinks, recent in ((1, 0, 0), (63, 2, 5), (64, 0, 64), (65, 65, 0), (200, 4, 30), (329, 1, 1), (330, 0, 3)):
+        lens = [0, 1, keep, min(keep + 1, L), L, 299]
+        cache = _cache(gen, 6, 2, L, d, dtype, lens, pos="mixed")
+        to = _cache(gen, 6, 2, keep + 3, d, dtype, [0] * 6) if into else None
+        _evict(cache, lens, keep, sinks, recent, to)
+
+
+@pytest.mark.parametrize("L", [40, 1000, 1030, 4096, 5000, 16385, 40000])
+@pytest.mark.parametrize("into", [False, True])
+def test_evict_of_every_length_class(L, into):
+    gen = _gen(L)
+    cache = _cache(gen, 1, 2, L, 16, I8, [L], pos=None)
+    keep = (L * 2) // 3
+    to = _cache(gen, 1, 2, keep, 16, I8, [0], pos="slots") if into else None
+    _evict(cache, None, keep, 3, keep // 4, to)
+
+
+@pytest.mark.parametrize("kind", ["equal", "zeros", "few", "special", "close"])
+@pytest.mark.parametrize("L", [500, 20000])
+def test_evict_ties_and_special_scores(kind, L):
+    """Equal scores go by slot, in one bin of a digit or all of them; zeros of both signs are equal; infinities; NaN below all."""
+    gen = _gen(11)
+    cache = _cache(gen, 2, 1, L, 16, BF16, [L, L - 77], pos="mixed")
+    s = torch.rand((2, 1, L), generator=gen)
+    if kind == "equal":
+        s.fill_(0.25)
+    elif kind == "zeros":
+        s = torch.where(s < 0.5, 0.0, -0.0)
+    elif kind == "few":
+        s = torch.floor(s * 3) - 1
+    elif kind == "close":
+        s = 1.0 + torch.floor(s * 4) * 2.0 ** -23
+    else:
+        s = torch.where(s < 0.2, float("nan"), torch.where(s < 0.4, float("-inf"), torch.where(s < 0.6, float("inf"), s - 0.8)))
+    cache.scores.copy_(s.to(DEV))
+    for keep, recent in ((L // 7, 0), (L // 2, 20), (L - L // 9, 3), (L - 10, 0)):
+        copy = llla.Cache(*(None if t is None else t.clone() for t in cache))
+        _evict(copy, [L, L - 77], keep, 0, recent)
+
+
+@pytest.mark.parametrize("dtype", [I8, E4M3])
+def test_evicted_rows_of_very_different_blocks(dtype):
+    """Rows that do not fit the exponent of the block they come into, and rows that do although their own block's is larger."""
+    gen = _gen(21)
+    for into in (False, True):
+        cache = _cache(gen, 2, 2, 700, 32, dtype, [700, 650], pos="mixed", spread=3.0)
+        to = llla.cache_alloc(2, 2, 300, 32, dtype, DEV, scores=True, pos=True) if into else None
+        _evict(cache, [700, 650], 300, 4, 16, to)
+
+
+def test_evict_marked_blocks():
+    """A row from a block that holds a value which is not finite marks the block it comes into; an e4m3 code that is no number does too."""
+    gen = _gen(31)
+    for dtype in (I8, E4M3):
+        cache = _cache(gen, 1, 2, 400, 32, dtype, [400], pos="mixed")
+        cache.k_exp[0, 0, 4] = -128
+        cache.v_exp[0, 1, 1] = -128
+        if dtype == E4M3:
+            ref.bits(cache.V)[0, 0, 390, 3] = 0x7f
+        to = llla.cache_alloc(1, 2, 150, 32, dtype, DEV, scores=True, pos=True)
+        _evict(llla.Cache(*(None if t is None else t.clone() for t in cache)), [400], 150, 0, 0, to)
+        _evict(cache, [400], 150, 0, 0)
+
+
+def test_evict_with_other_strides_and_without_pos():
+    gen = _gen(41)
+    for dtype in (I8, BF16, F32):
+        c = _cache(gen, 2, 3, 300, 64, dtype, [300, 290], pos=None)
+        cache = c._replace(K=_padded(c.K, 16), V=_padded(c.V, 48))
+        _evict(cache, [300, 290], 111, 2, 9)
+
+
+def test_protected_positions_that_repeat():
+    """More rows are protected than stay (positions that repeat): the lower slots stay, and there are never more than `keep`."""
+    gen = _gen(51)
+    cache = _cache(gen, 1, 2, 200, 16, BF16, [200], pos="slots")
+    cache.pos.fill_(3)
+    _evict(cache, [200], 50, 10, 5)
+
+
+def test_last_bits_of_a_very_long_cache():
+    """Offsets beyond 2^31 bytes: rows of a cache of 4.3 GB, appended to, evicted in place."""
+    L, H, d = 1 << 21, 8, 128
+    cache = llla.cache_alloc(1, H, L, d, BF16, DEV, scores=True)
+    n = 37
+    gen = _gen(61)
+    k, v = _rows(gen, (1, H, n, d)).to(BF16).to(DEV), _rows(gen, (1, H, n, d)).to(BF16).to(DEV)
+    lens = torch.tensor([L - n], dtype=torch.int32, device=DEV)
+    llla.llla_cache_append(cache, k, v, seqlens=lens)
+    assert torch.equal(cache.K[0, :, L - n:], k[0]) and torch.equal(cache.V[0, :, L - n:], v[0])
+    cache.scores[:, :, L - n:] = 5.0
+    cache.scores[:, :, 100:L - n] = 1.0
+    got = llla.llla_cache_evict(cache, L - n)
+    torch.cuda.synchronize()
+    assert got.item() == L - n
+    # slots 0 .. 99 have score 0: the last of them are given up
+    assert torch.equal(cache.K[0, :, 100 - n:100], k[0]) and torch.equal(cache.V[0, :, 100 - n:100], v[0])
+    assert not cache.K[0, :, :100 - n].any() and torch.equal(cache.scores[0, :, 100 - n:100], torch.full((H, n), 5.0, device=DEV))
