@@ -226,20 +226,31 @@ hipError_t append_by_input(const AppendProblem &p)
 }
 
 // ---- evict: what stays --------------------------------------------------------------------------------------------------------------
-// Workspace of one (sequence, head), in 32-bit words: header, sources, and in place also destinations and the first hole of each block
+// Workspace of one (sequence, head), in 32-bit words: header, sources, and in place also destinations and the first hole of each block;
+// for long caches also what the launches of the selection hand on
 struct EvictPlan {
     int most;              // moves at most
     int blocks;            // in place: blocks of destinations
+    int chunks;            // workgroups of a head, 0: one for the head
+    int state;             // offset of the state of the selection
     int words;
 };
 constexpr int PLAN_HDR = 4;                               // moves, exponents of the block that holds slot `keep`
+constexpr int BINS = 2048, HISTS = 3 * BINS, CHOICES = 4 * 5;      // histograms, and the choice of each step
+
+constexpr int CHUNK = 2048;                               // slots of a workgroup where a head has several
+// One workgroup holds up to 8192 ranks in registers and selects in one launch; longer rows take six launches of many.  us, one workgroup / six
+// launches (LDS histograms and ranks formed anew from memory in every pass of the former beyond 32768): see evict_plan_kernel.
+constexpr int ONE_LAUNCH = 16384;
 
 inline EvictPlan evict_plan(int L_max, int keep, bool in_place)
 {
     EvictPlan p;
     p.most = in_place ? std::min(keep, L_max - keep) : keep;
     p.blocks = in_place ? cache_blocks(keep) : 0;
-    p.words = (PLAN_HDR + p.most + (in_place ? p.most + p.blocks + 1 : 0) + 63) / 64 * 64;
+    p.chunks = L_max <= ONE_LAUNCH ? 0 : (L_max + CHUNK - 1) / CHUNK;
+    p.state = PLAN_HDR + p.most + (in_place ? p.most + p.blocks + 1 : 0);
+    p.words = (p.state + (p.chunks ? HISTS + CHOICES + 5 * p.chunks : 0) + 63) / 64 * 64;
     return p;
 }
 
@@ -263,189 +274,395 @@ __device__ __forceinline__ unsigned rank_of(float s)
     return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// The `keep` best rows of a head, and where they go.  A radix select of three digits (11, 11, 10 bits; eleven so that scores of similar size spread over
-// many bins) finds the rank T of the last row that stays and how many rows of that rank do; a row's place follows from counts per
-// wave of the rows that stay, or are holes (slot < keep, given up) or movers (slot >= keep, kept) in front of it.  Wave w owns a run of whole
-// groups of 64 slots, so ballots count in the order of the slots, which decides between equal ranks.
-// KPT > 0: the ranks of KPT groups per wave stay in registers; KPT == 0: any length, ranks are formed again in every pass.
+__device__ __forceinline__ int wave_max_int(int x)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) x = max(x, __shfl_xor(x, off));
+    return x;
+}
+
+__device__ __forceinline__ int popcount64(uint64_t m) { return __builtin_popcountll(m); }
+
+// One head as a workgroup sees it
+struct EvictHead {
+    int bh, len;
+    const float *scores;
+    const int32_t *pos;
+    int *hdr, *src, *dst, *hole_of, *state;
+    __device__ EvictHead(const EvictArgs &a, int bh_) : bh(bh_)
+    {
+        len = cache_length(a.seqlens, bh / a.H, a.L_max);
+        scores = a.scores + (size_t)bh * a.L_max;
+        pos = a.pos ? a.pos + (size_t)bh * a.L_max : nullptr;
+        hdr = a.ws + (size_t)bh * a.plan.words;
+        src = hdr + PLAN_HDR;
+        dst = src + a.plan.most;
+        hole_of = dst + a.plan.most;
+        state = hdr + a.plan.state;
+    }
+};
+
+// Positions and scores of KPT groups of 64 slots, as ranks.  (Every load has a valid address and no condition around it, so that all are in flight
+// together: with a condition each was waited for, 16 trips to memory one after the other, 34 us for 256 heads of 4160 rows.)
+template <int KPT>
+struct Ranks {
+    unsigned own[KPT];
+    int p[KPT];
+    __device__ void load(const EvictHead &x, int first, int lane)
+    {
+        const int last = x.len - 1;
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) own[i] = __float_as_uint(x.scores[min(first + 64 * i + lane, last)]);
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) p[i] = x.pos ? x.pos[min(first + 64 * i + lane, last)] : first + 64 * i + lane;
+    }
+    __device__ int newest(const EvictHead &x, int first, int lane) const
+    {
+        int m = INT32_MIN;
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) m = first + 64 * i + lane < x.len ? max(m, p[i]) : m;
+        return wave_max_int(m);
+    }
+    __device__ void rank(const EvictArgs &a, int newest)
+    {
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            const bool safe = p[i] < a.sinks || (a.recent > 0 && (int64_t)p[i] > (int64_t)newest - a.recent);
+            own[i] = safe ? SAFE : rank_of(__uint_as_float(own[i]));
+        }
+    }
+};
+
+// Digits of a rank: 11, 11 and 10 bits; eleven so that scores of similar size spread over many bins
+__device__ __forceinline__ int digit_shift(int digit) { return digit == 0 ? 21 : digit == 1 ? 10 : 0; }
+__device__ __forceinline__ unsigned digit_mask(int digit) { return digit == 2 ? 1023u : 2047u; }
+
+// What is known of the rank T of the last row that stays: rows above T stay, and the first `need` of rank T
+struct Choice {
+    unsigned T;
+    int need;
+    bool done;             // T is final
+};
+
+// Narrows the choice by the histogram of the digit, of which a thread has its own PER bins, counted from the top.  All threads of the workgroup;
+// pick, wsum: LDS.
+template <int THREADS>
+struct Bins {
+    static constexpr int PER = BINS / THREADS;
+    unsigned v[PER];
+    __device__ void load(const unsigned *hist)
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] = hist[BINS - 1 - (PER * (int)threadIdx.x + i)];
+    }
+};
+template <int THREADS>
+__device__ __forceinline__ void narrow(Choice &c, int digit, const Bins<THREADS> &b, unsigned *wsum, int *pick)
+{
+    constexpr int NW = THREADS / 64, PER = Bins<THREADS>::PER;
+    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const auto &bin = b.v;
+    unsigned mine = 0u;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) mine += bin[i];
+    unsigned incl = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const unsigned y = (unsigned)__shfl_up((int)incl, off);
+        if (lane >= off) incl += y;
+    }
+    if (lane == 63) wsum[wave] = incl;
+    __syncthreads();
+    unsigned above = incl - mine;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) above += w < wave ? wsum[w] : 0u;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (above < (unsigned)c.need && above + bin[i] >= (unsigned)c.need) {      // one bin of one thread
+            pick[0] = BINS - 1 - (PER * tid + i);
+            pick[1] = (int)above;
+            pick[2] = (int)bin[i];
+        }
+        above += bin[i];
+    }
+    __syncthreads();
+    c.T |= (unsigned)pick[0] << digit_shift(digit);
+    c.need -= pick[1];
+    if (digit < 2 && pick[2] == c.need && c.T > 0u) {      // all rows of the bin stay: those above the rank in front of it (one of zero never does)
+        c.T -= 1u;
+        c.need = 0;
+        c.done = true;
+    }
+    __syncthreads();                                      // (pick is free again)
+}
+
+template <int KPT>
+__device__ __forceinline__ void count_digit(const Ranks<KPT> &r, const EvictHead &x, int first, int lane, int digit, const Choice &c, unsigned *hist)
+{
+    const int shift = digit_shift(digit), before = digit == 1 ? 21 : 10;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        const bool in = first + 64 * i + lane < x.len && (digit == 0 || r.own[i] >> before == c.T >> before);
+        if (in) atomicAdd(&hist[(r.own[i] >> shift) & digit_mask(digit)], 1u);
+    }
+}
+
+// A group of 64 slots as bit masks: rows above T, rows at T, slots below `keep`.  Scalar, like all that is counted from them.
+struct Group { uint64_t gt, eq, low; };
+template <int KPT>
+__device__ __forceinline__ Group group_of(const Ranks<KPT> &r, const EvictHead &x, int i, int first, int lane, int keep, bool all, const Choice &c)
+{
+    const int s0 = first + 64 * i;
+    auto bits = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; };
+    const uint64_t live = bits(x.len - s0);
+    if (all) return Group{live, 0ull, bits(keep - s0)};
+    return Group{live & __builtin_amdgcn_ballot_w64(r.own[i] > c.T), live & __builtin_amdgcn_ballot_w64(r.own[i] == c.T), bits(keep - s0)};
+}
+
+// rows above T and at T, each below slot keep and from there on
+struct Counts { int gl, gh, el, eh; };
+template <int KPT>
+__device__ __forceinline__ Counts count_sides(const Ranks<KPT> &r, const EvictHead &x, int first, int lane, int keep, bool all, const Choice &c)
+{
+    Counts n{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        if (first + 64 * i < x.len) {                     // (a scalar branch)
+            const Group g = group_of(r, x, i, first, lane, keep, all, c);
+            n.gl += popcount64(g.gt & g.low);
+            n.gh += popcount64(g.gt & ~g.low);
+            n.el += popcount64(g.eq & g.low);
+            n.eh += popcount64(g.eq & ~g.low);
+        }
+    }
+    return n;
+}
+
+// Rows in front of a run of slots: of rank T; that stay, by side of slot keep
+struct Front { int equal, low, high; };
+__device__ __forceinline__ void advance(Front &f, const Counts &n, int need)
+{
+    const int tl = min(max(need - f.equal, 0), n.el), th = min(max(need - f.equal - n.el, 0), n.eh);
+    f.equal += n.el + n.eh;
+    f.low += n.gl + tl;
+    f.high += n.gh + th;
+}
+
+// number of a mask's bits below the lane
+__device__ __forceinline__ int bits_below(uint64_t m)
+{
+    return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u));
+}
+
+// A row's place follows from the rows in front of it that stay, or are holes (slot < keep, given up) or movers (slot >= keep, kept)
+template <int KPT>
+__device__ __forceinline__ void place(const EvictArgs &a, const EvictHead &x, const Ranks<KPT> &r, int first, int lane, bool all, const Choice &c, Front f,
+                                      bool last)
+{
+    const int keep = a.keep;
+    int kept = f.low + f.high, holes = min(min(first, keep), x.len) - f.low, movers = f.high, equal = f.equal;
+    auto mine = [&](uint64_t m) { return ((m >> lane) & 1) != 0; };
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        const int s0 = first + 64 * i, s = s0 + lane;
+        if (s0 < x.len) {                                 // (scalar branches)
+            const Group g = group_of(r, x, i, first, lane, keep, all, c);
+            uint64_t stay = g.gt;
+            if (g.eq != 0) {
+                if (equal < c.need) stay |= g.eq & __builtin_amdgcn_ballot_w64(equal + bits_below(g.eq) < c.need);
+                equal += popcount64(g.eq);
+            }
+            if (!a.in_place) {
+                if (mine(stay)) {
+                    const int j = kept + bits_below(stay);
+                    x.src[j] = s;
+                    if (a.index) a.index[(size_t)x.bh * keep + j] = s;
+                }
+                kept += popcount64(stay);
+            } else {
+                const uint64_t hole = ~stay & g.low, mover = stay & ~g.low;      // (more rows than keep: the slots below it are all taken)
+                if (lane == 0 && s0 / 64 < a.plan.blocks) x.hole_of[s0 / 64] = holes;
+                if (mine(hole)) x.dst[holes + bits_below(hole)] = s;
+                if (mine(mover)) x.src[movers + bits_below(mover)] = s;
+                if (a.index && mine(stay & g.low)) a.index[(size_t)x.bh * keep + s] = s;
+                holes += popcount64(hole);
+                movers += popcount64(mover);
+            }
+        }
+    }
+    if (last && lane == 0) {                              // (the last run's counts end with all rows)
+        x.hdr[0] = a.in_place ? movers : kept;
+        if (a.in_place) {
+            x.hole_of[a.plan.blocks] = holes;
+            if (a.ke) {
+                const size_t at = (size_t)x.bh * cache_blocks(a.L_max) + keep / CACHE_BLOCK;      // (more rows than keep: the slot exists)
+                x.hdr[1] = a.ke[at];
+                x.hdr[2] = a.ve[at];
+            }
+        }
+    }
+}
+
+// Lengths, and heads that have nothing to select; true: done
+template <int THREADS>
+__device__ __forceinline__ bool evict_early(const EvictArgs &a, const EvictHead &x)
+{
+    const int tid = threadIdx.x;
+    if (x.bh % a.H == 0 && tid == 0) a.lens[x.bh / a.H] = min(x.len, a.keep);
+    if (x.len == 0 || (a.in_place && x.len <= a.keep)) {
+        if (tid == 0) x.hdr[0] = 0;
+        for (int t = tid; a.in_place && t <= a.plan.blocks; t += THREADS) x.hole_of[t] = 0;
+        if (a.index)
+            for (int j = tid; j < x.len; j += THREADS) a.index[(size_t)x.bh * a.keep + j] = j;
+        return true;
+    }
+    return false;
+}
+
+// The `keep` best rows of a head, and where they go: a radix select finds the rank of the last row that stays, then every row's place follows from
+// counts per wave.  Wave w owns a run of whole groups of 64 slots, so ballots count in the order of the slots, which decides between equal ranks.
 template <int THREADS, int KPT>
 __global__ __launch_bounds__(THREADS) void evict_plan_kernel(EvictArgs a)
 {
-    constexpr int NW = THREADS / 64, BINS = 2048, PER = BINS / THREADS;
+    constexpr int NW = THREADS / 64;
     __shared__ unsigned hist[BINS];
     __shared__ unsigned wsum[NW];
-    __shared__ int pick[2];                               // digit of T, rows of higher digits
+    __shared__ int pick[3];
     __shared__ int newest_s[NW];
-    __shared__ int counts[NW][4];                         // rows above T and at T, each below slot keep and from there on
+    __shared__ Counts counts[NW];
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-    const int bh = blockIdx.x, b = bh / a.H;
-    const int len = cache_length(a.seqlens, b, a.L_max), keep = a.keep;
-    const float *scores = a.scores + (size_t)bh * a.L_max;
-    const int32_t *pos = a.pos ? a.pos + (size_t)bh * a.L_max : nullptr;
-    int *hdr = a.ws + (size_t)bh * a.plan.words, *src = hdr + PLAN_HDR, *dst = src + a.plan.most, *hole_of = dst + a.plan.most;
-    if (bh % a.H == 0 && tid == 0) a.lens[b] = min(len, keep);
-    if (a.in_place && len <= keep) {                      // nothing to give up
-        if (tid == 0) hdr[0] = 0;
-        for (int t = tid; t <= a.plan.blocks; t += THREADS) hole_of[t] = 0;
-        if (a.index)
-            for (int j = tid; j < len; j += THREADS) a.index[(size_t)bh * keep + j] = j;
-        return;
-    }
-    const int groups = KPT > 0 ? KPT : (a.L_max + 64 * NW - 1) / (64 * NW), first = wave * groups * 64;
-
-    int newest = len - 1;
-    if (pos && a.recent > 0) {
-        int m = INT32_MIN;
-        for (int i = 0; i < groups; ++i) {
-            const int s = first + 64 * i + lane;
-            if (s < len) m = max(m, pos[s]);
-        }
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) m = max(m, __shfl_xor(m, off));
+    const EvictHead x(a, blockIdx.x);
+    if (evict_early<THREADS>(a, x)) return;
+    const int first = wave * KPT * 64;
+    Ranks<KPT> r;
+    r.load(x, first, lane);
+    int newest = x.len - 1;
+    if (x.pos && a.recent > 0) {
+        const int m = r.newest(x, first, lane);
         if (lane == 0) newest_s[wave] = m;
         __syncthreads();
         newest = INT32_MIN;
 #pragma unroll
         for (int w = 0; w < NW; ++w) newest = max(newest, newest_s[w]);
     }
-    auto rank_at = [&](int s) {
-        const int p = pos ? pos[s] : s;
-        return p < a.sinks || (a.recent > 0 && (int64_t)p > (int64_t)newest - a.recent) ? SAFE : rank_of(scores[s]);
-    };
-    unsigned own[KPT > 0 ? KPT : 1];
-    if constexpr (KPT > 0) {
-#pragma unroll
-        for (int i = 0; i < KPT; ++i) {
-            const int s = first + 64 * i + lane;
-            own[i] = s < len ? rank_at(s) : 0u;
+    r.rank(a, newest);
+    const bool all = x.len <= a.keep;
+    Choice c{0u, a.keep, all};
+#pragma unroll 1
+    for (int digit = 0; digit < 3 && !c.done; ++digit) {
+        for (int i = tid; i < BINS; i += THREADS) hist[i] = 0u;
+        __syncthreads();
+        count_digit(r, x, first, lane, digit, c, hist);
+        __syncthreads();
+        Bins<THREADS> bins;
+        bins.load(hist);
+        narrow<THREADS>(c, digit, bins, wsum, pick);
+    }
+    const Counts n = count_sides(r, x, first, lane, a.keep, all, c);
+    if (lane == 0) counts[wave] = n;
+    __syncthreads();
+    Front f{0, 0, 0};
+    for (int w = 0; w < wave; ++w) advance(f, counts[w], c.need);
+    place(a, x, r, first, lane, all, c, f, wave == NW - 1);
+}
+
+// The same for long caches, a head dealt over workgroups of CHUNK slots, in six launches: step 0 newest positions (and histograms cleared), 1 to 3 the
+// digits, 4 counts, 5 places.  Every workgroup reads the histogram of the step before and narrows the choice for itself.
+// state: histograms, choice of each step, newest position of each chunk, counts of each chunk
+__global__ __launch_bounds__(NT) void evict_long_kernel(EvictArgs a, int step)
+{
+    constexpr int KPT = CHUNK / NT, NWG = NT / 64;
+    __shared__ unsigned hist[BINS];
+    __shared__ unsigned wsum[NWG];
+    __shared__ int pick[3];
+    __shared__ Counts counts[NWG];
+    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), chunk = blockIdx.x;
+    const EvictHead x(a, blockIdx.y);
+    int *choice_of = x.state + HISTS, *newest_of = choice_of + CHOICES;
+    Counts *counts_of = reinterpret_cast<Counts *>(newest_of + a.plan.chunks);
+    unsigned *hists = reinterpret_cast<unsigned *>(x.state);
+    if (step == 0) {
+        for (int i = chunk * NT + tid; i < HISTS; i += a.plan.chunks * NT) hists[i] = 0u;
+        if (chunk == 0) evict_early<NT>(a, x);
+    }
+    if (x.len == 0 || (a.in_place && x.len <= a.keep)) return;
+    const int first = chunk * CHUNK + wave * KPT * 64;
+    const bool all = x.len <= a.keep, live = chunk * CHUNK < x.len;
+    Ranks<KPT> r;
+    if (step == 0) {
+        if (!x.pos || a.recent == 0) return;
+        r.load(x, first, lane);
+        const int m = r.newest(x, first, lane);
+        if (lane == 0) wsum[wave] = (unsigned)m;
+        __syncthreads();
+        if (tid == 0) newest_of[chunk] = max(max((int)wsum[0], (int)wsum[1]), max((int)wsum[2], (int)wsum[3]));
+        return;
+    }
+    if (!live && step < 3) return;
+    // what the step reads, all requested together: a trip to memory is a fifth of it
+    r.load(x, first, lane);
+    Bins<NT> bins;
+    bins.load(hists + (step < 2 ? 0 : min(step - 2, 2)) * BINS);
+    const bool by_age = x.pos && a.recent > 0;
+    int newest = INT32_MIN;
+    if (by_age) newest = newest_of[min(lane, a.plan.chunks - 1)];
+    const int *before = choice_of + 4 * (step - 1);
+    const Choice told{(unsigned)before[0], before[1], before[2] != 0};
+    const bool placed = choice_of[4 * 3 + 2] != 0;
+    // The choice that the step before began with, narrowed by what it counted.  Ordinarily two digits tell (scores differ): step 3 then counts the rows that
+    // stay, step 4 gives them their places, and the last step has nothing left to do.
+    if (step == 5 && placed) return;
+    Choice c = step <= 2 ? Choice{0u, a.keep, all} : told;
+    const bool counted = step == 5 || (step == 4 && c.done);
+    if (step >= 2 && step <= 4) {
+        if (!c.done) {
+            narrow<NT>(c, step - 2, bins, wsum, pick);
+        }
+        if (chunk == 0 && tid == 0) {
+            choice_of[4 * step] = (int)c.T;
+            choice_of[4 * step + 1] = c.need;
+            choice_of[4 * step + 2] = c.done ? 1 : 0;
         }
     }
-    auto for_groups = [&](auto fn) {                      // fn(slot, live, rank), in order
-        if constexpr (KPT > 0) {
-#pragma unroll
-            for (int i = 0; i < KPT; ++i) {
-                const int s = first + 64 * i + lane;
-                fn(s, s < len, own[i]);
-            }
-        } else {
-            for (int i = 0; i < groups; ++i) {
-                const int s = first + 64 * i + lane;
-                if (first + 64 * i >= len) break;
-                fn(s, s < len, s < len ? rank_at(s) : 0u);
-            }
-        }
-    };
-
-    // the rank T of the keep-th best row; `need` of the rows of that rank stay
-    const bool all = len <= keep;
-    unsigned T = 0u;
-    int need = keep;
-    if (!all) {
-#pragma unroll
-        for (int digit = 0; digit < 3; ++digit) {
-            const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0;
-            const unsigned mask = digit == 2 ? 1023u : 2047u;
-            for (int i = tid; i < BINS; i += THREADS) hist[i] = 0u;
-            __syncthreads();
-            for_groups([&](int, bool live, unsigned r) {
-                const bool in = digit == 0 || (r >> (digit == 1 ? 21 : 10)) == (T >> (digit == 1 ? 21 : 10));
-                if (live && in) atomicAdd(&hist[(r >> shift) & mask], 1u);
-            });
-            __syncthreads();
-            // rows in the bins above this thread's, which are PER (tid ..) counted from the top
-            unsigned mine = 0u, bin[PER];
-#pragma unroll
-            for (int i = 0; i < PER; ++i) { bin[i] = hist[BINS - 1 - (PER * tid + i)]; mine += bin[i]; }
-            unsigned incl = mine;
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const unsigned y = (unsigned)__shfl_up((int)incl, off);
-                if (lane >= off) incl += y;
-            }
-            if (lane == 63) wsum[wave] = incl;
-            __syncthreads();
-            unsigned above = incl - mine;
-#pragma unroll
-            for (int w = 0; w < NW; ++w) above += w < wave ? wsum[w] : 0u;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                if (above < (unsigned)need && above + bin[i] >= (unsigned)need) {      // one bin of one thread
-                    pick[0] = BINS - 1 - (PER * tid + i);
-                    pick[1] = (int)above;
-                }
-                above += bin[i];
-            }
-            __syncthreads();
-            T |= (unsigned)pick[0] << shift;
-            need -= pick[1];
-        }
+    for (int i = lane + 64; by_age && i < a.plan.chunks; i += 64) newest = max(newest, newest_of[i]);
+    r.rank(a, by_age ? wave_max_int(newest) : x.len - 1);
+    if (step <= 2 || (step == 3 && !c.done)) {
+        if (c.done || !live) return;
+        for (int i = tid; i < BINS; i += NT) hist[i] = 0u;
+        __syncthreads();
+        count_digit(r, x, first, lane, step - 1, c, hist);
+        __syncthreads();
+        for (int i = tid; i < BINS; i += NT)
+            if (hist[i]) atomicAdd(&hists[(step - 1) * BINS + i], hist[i]);
+        return;
     }
-
-    // rows per wave, below slot keep and from there on
+    const Counts n = count_sides(r, x, first, lane, a.keep, all, c);
+    if (lane == 0) counts[wave] = n;
+    __syncthreads();
+    if (!counted) {
+        if (tid == 0) {
+            Counts s = counts[0];
+            for (int w = 1; w < NWG; ++w) { s.gl += counts[w].gl; s.gh += counts[w].gh; s.el += counts[w].el; s.eh += counts[w].eh; }
+            counts_of[chunk] = s;
+        }
+        return;
+    }
+    // what is in front of the chunk: sums of the chunks, those of rank T that stay as one run below slot keep and one from there on
+    Front f{0, 0, 0};
     {
         int gl = 0, gh = 0, el = 0, eh = 0;
-        for_groups([&](int s, bool live, unsigned r) {
-            const bool gt = live && (all || r > T), eq = live && !all && r == T;
-            gl += __builtin_popcountll(__builtin_amdgcn_ballot_w64(gt && s < keep));
-            gh += __builtin_popcountll(__builtin_amdgcn_ballot_w64(gt && s >= keep));
-            el += __builtin_popcountll(__builtin_amdgcn_ballot_w64(eq && s < keep));
-            eh += __builtin_popcountll(__builtin_amdgcn_ballot_w64(eq && s >= keep));
-        });
-        if (lane == 0) { counts[wave][0] = gl; counts[wave][1] = gh; counts[wave][2] = el; counts[wave][3] = eh; }
-    }
-    __syncthreads();
-    int equal = 0, kept = 0, kept_high = 0, kept_low = 0; // in front of this wave: rows of rank T; rows that stay, also by side
-    {
-        int e = 0;
-        for (int w = 0; w < NW; ++w) {
-            const int el = counts[w][2], eh = counts[w][3];
-            const int tl = min(max(need - e, 0), el), th = min(max(need - e - el, 0), eh);
-            if (w < wave) {
-                equal += el + eh;
-                kept_low += counts[w][0] + tl;
-                kept_high += counts[w][1] + th;
-            }
-            e += el + eh;
+        for (int i = lane; i < chunk; i += 64) {
+            const Counts k = counts_of[i];
+            gl += k.gl; gh += k.gh; el += k.el; eh += k.eh;
         }
-        kept = kept_low + kept_high;
-    }
-    int holes = min(min(first, keep), len) - kept_low, movers = kept_high;
-    const uint64_t below = (1ull << lane) - 1;
-    for_groups([&](int s, bool live, unsigned r) {
-        const bool eq = live && !all && r == T;
-        const uint64_t me = __builtin_amdgcn_ballot_w64(eq);
-        const bool stays = live && (all || r > T || (eq && equal + __builtin_popcountll(me & below) < need));
-        equal += __builtin_popcountll(me);
-        if (!a.in_place) {
-            const uint64_t m = __builtin_amdgcn_ballot_w64(stays);
-            if (stays) {
-                const int j = kept + __builtin_popcountll(m & below);
-                src[j] = s;
-                if (a.index) a.index[(size_t)bh * keep + j] = s;
-            }
-            kept += __builtin_popcountll(m);
-        } else {
-            const bool hole = live && !stays && s < keep, mover = stays && s >= keep;
-            const uint64_t mh = __builtin_amdgcn_ballot_w64(hole), mm = __builtin_amdgcn_ballot_w64(mover);
-            if (lane == 0 && s / 64 < a.plan.blocks) hole_of[s / 64] = holes;
-            if (hole) dst[holes + __builtin_popcountll(mh & below)] = s;
-            if (mover) src[movers + __builtin_popcountll(mm & below)] = s;
-            if (a.index && stays && s < keep) a.index[(size_t)bh * keep + s] = s;
-            holes += __builtin_popcountll(mh);
-            movers += __builtin_popcountll(mm);
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) {
+            gl += __shfl_xor(gl, off); gh += __shfl_xor(gh, off); el += __shfl_xor(el, off); eh += __shfl_xor(eh, off);
         }
-    });
-    if (wave == NW - 1 && lane == 0) {                    // (the last wave's counts end with all rows)
-        hdr[0] = a.in_place ? movers : kept;
-        if (a.in_place) {
-            hole_of[a.plan.blocks] = holes;
-            if (a.ke) {
-                const size_t at = (size_t)bh * cache_blocks(a.L_max) + keep / CACHE_BLOCK;      // (len > keep: the slot exists)
-                hdr[1] = a.ke[at];
-                hdr[2] = a.ve[at];
-            }
-        }
+        advance(f, Counts{gl, gh, el, eh}, c.need);
     }
+    for (int w = 0; w < wave; ++w) advance(f, counts[w], c.need);
+    place(a, x, r, first, lane, all, c, f, chunk == a.plan.chunks - 1 && wave == NWG - 1);
 }
 
 // ---- evict: rows that move ----------------------------------------------------------------------------------------------------------
@@ -501,91 +718,126 @@ __global__ __launch_bounds__(NT) void move_kernel(MoveArgs a)
     if (tid < count) move_row_words(a, bh, src[i0 + tid], a.in_place ? dst[i0 + tid] : i0 + tid);
 }
 
-// Rows of codes: one workgroup per block of destinations.  A row needs the exponent that its own largest code asks for, not its old block's, so a
-// block's exponent only grows for rows that do not fit it.
+// Exponent that sixteen codes of exponent e ask for (EXP_LEAST for zeros).  A row needs the exponent that its own largest code asks for, not its
+// old block's, so a block's exponent only grows for rows that do not fit it.
+template <typename F>
+__device__ __forceinline__ int exponent_needed(uint4 w, int e)
+{
+    const unsigned v[4] = {w.x, w.y, w.z, w.w};
+    unsigned m = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float x[4];
+        decode4<F>(v[i], x);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) m = max(m, abs_bits(x[t]));
+    }
+    if (e == EXP_NAN) return EXP_NAN;
+    if (m == 0u) return EXP_LEAST;
+    const int n = exponent_of<F>(__uint_as_float(m));
+    return n == EXP_NAN ? EXP_NAN : max(n + e, EXP_LEAST);
+}
+
+__device__ __forceinline__ int wave_join(int e)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) e = exponent_join(e, __shfl_xor(e, off));
+    return e;
+}
+
+// Rows of codes into another cache: one workgroup per block of destinations
 template <int D, typename F>
 __global__ __launch_bounds__(NT) void move_codes_kernel(MoveArgs a)
 {
     using U = Units<D>;
-    __shared__ int from_s[CACHE_BLOCK];
     __shared__ int needs[2][NT / 64];
     const int tid = threadIdx.x, bh = blockIdx.y, b = bh / a.H, h = bh % a.H, blk = blockIdx.x, base = blk * CACHE_BLOCK;
-    const int *hdr = a.ws + (size_t)bh * a.plan.words, *src = hdr + PLAN_HDR, *dst = src + a.plan.most, *hole_of = dst + a.plan.most;
-    int i0 = base, count;
-    if (a.in_place) {
-        i0 = hole_of[blk];
-        count = hole_of[blk + 1] - i0;
-    } else {
-        count = min(hdr[0] - base, CACHE_BLOCK);
-    }
+    const int *hdr = a.ws + (size_t)bh * a.plan.words, *src = hdr + PLAN_HDR;
+    const int count = min(hdr[0] - base, CACHE_BLOCK);
     if (count <= 0) return;
-    if (tid < CACHE_BLOCK) from_s[tid] = -1;
-    __syncthreads();
-    if (tid < count) {
-        const int s = src[i0 + tid], d = a.in_place ? dst[i0 + tid] : i0 + tid;
-        from_s[d - base] = s;
-        move_row_words(a, bh, s, d);
-    }
-    __syncthreads();
+    if (tid < count) move_row_words(a, bh, src[base + tid], base + tid);
     const size_t exps = (size_t)bh * cache_blocks(a.L_max);
     uint4 w[U::ITER];
-    int from[U::ITER], e0[U::ITER];
+    int e0[U::ITER];
     int need[2] = {EXP_LEAST, EXP_LEAST};
 #pragma unroll
     for (int it = 0; it < U::ITER; ++it) {
         const U u(it, tid);
-        from[it] = -1;
-        if (!U::PARTIAL || tid < U::ALL) from[it] = from_s[u.row];
-        unsigned m = 0u;
-        e0[it] = EXP_LEAST;
-        if (from[it] >= 0) {
-            const llla_strides &ss = u.tensor ? a.sv : a.sk;
-            w[it] = *reinterpret_cast<const uint4 *>(static_cast<const int8_t *>(u.tensor ? a.V : a.K) + b * ss.batch + h * ss.head +
-                                                     (int64_t)from[it] * ss.seq + 16 * u.part);
-            // (in place the block of slot keep may be getting another exponent in these moments: as the plan saw it)
-            const int fb = from[it] / CACHE_BLOCK;
-            e0[it] = a.in_place && fb == a.keep / CACHE_BLOCK ? hdr[1 + u.tensor] : (int)(u.tensor ? a.ve : a.ke)[exps + fb];
-            const unsigned v[4] = {w[it].x, w[it].y, w[it].z, w[it].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float x[4];
-                decode4<F>(v[i], x);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) m = max(m, abs_bits(x[t]));
-            }
-        }
-        // of these sixteen codes; the block takes the largest anyway
-        int n = m == 0u ? EXP_LEAST : exponent_of<F>(__uint_as_float(m));
-        if (e0[it] == EXP_NAN) n = EXP_NAN;
-        else if (n != EXP_NAN && m != 0u) n = max(n + e0[it], EXP_LEAST);
-        need[0] = u.tensor ? need[0] : exponent_join(need[0], n);
-        need[1] = u.tensor ? exponent_join(need[1], n) : need[1];
+        const bool mine = (!U::PARTIAL || tid < U::ALL) && u.row < count;
+        const int from = src[base + min(u.row, count - 1)], tensor = u.tensor & 1;       // (a valid row without a condition)
+        const llla_strides &ss = tensor ? a.sv : a.sk;
+        w[it] = *reinterpret_cast<const uint4 *>(static_cast<const int8_t *>(tensor ? a.V : a.K) + b * ss.batch + h * ss.head +
+                                                 (int64_t)from * ss.seq + 16 * u.part);
+        e0[it] = (tensor ? a.ve : a.ke)[exps + from / CACHE_BLOCK];
+        const int n = mine ? exponent_needed<F>(w[it], e0[it]) : EXP_LEAST;
+        need[0] = tensor ? need[0] : exponent_join(need[0], n);
+        need[1] = tensor ? exponent_join(need[1], n) : need[1];
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) need[t] = exponent_join(need[t], __shfl_xor(need[t], off));
+        need[t] = wave_join(need[t]);
         if (tid % 64 == 0) needs[t][tid / 64] = need[t];
     }
-    const size_t at = (size_t)bh * cache_blocks(a.Ld_max) + blk;
-    int was[2] = {EXP_LEAST, EXP_LEAST};
-    if (a.in_place) { was[0] = a.ked[at]; was[1] = a.ved[at]; }
-    __syncthreads();                                      // (and the old exponents are read)
+    __syncthreads();
     int now[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-        now[t] = exponent_join(was[t], exponent_join(exponent_join(needs[t][0], needs[t][1]), exponent_join(needs[t][2], needs[t][3])));
-    if (tid < 2) (tid ? a.ved : a.ked)[at] = (int8_t)(tid ? now[1] : now[0]);
+    for (int t = 0; t < 2; ++t) now[t] = exponent_join(exponent_join(needs[t][0], needs[t][1]), exponent_join(needs[t][2], needs[t][3]));
+    if (tid < 2) (tid ? a.ved : a.ked)[(size_t)bh * cache_blocks(a.Ld_max) + blk] = (int8_t)(tid ? now[1] : now[0]);
 #pragma unroll
     for (int it = 0; it < U::ITER; ++it) {
         const U u(it, tid);
-        if (U::PARTIAL && tid >= U::ALL) break;
-        const int slot = base + u.row, e = u.tensor ? now[1] : now[0], eb = u.tensor ? was[1] : was[0];
+        if ((U::PARTIAL && tid >= U::ALL) || u.row >= count) continue;
+        const int e = u.tensor ? now[1] : now[0];
         const llla_strides &ds = u.tensor ? a.dv : a.dk;
-        uint4 *p = reinterpret_cast<uint4 *>(static_cast<int8_t *>(u.tensor ? a.Vd : a.Kd) + b * ds.batch + h * ds.head + (int64_t)slot * ds.seq + 16 * u.part);
-        if (from[it] >= 0) *p = e == EXP_NAN || e == e0[it] ? w[it] : shift16<F>(w[it], e0[it], e);
-        else if (a.in_place && slot < a.keep && e != eb && e != EXP_NAN) *p = shift16<F>(*p, eb, e);
+        *reinterpret_cast<uint4 *>(static_cast<int8_t *>(u.tensor ? a.Vd : a.Kd) + b * ds.batch + h * ds.head + (int64_t)(base + u.row) * ds.seq + 16 * u.part) =
+            e == EXP_NAN || e == e0[it] ? w[it] : shift16<F>(w[it], e0[it], e);
     }
+}
+
+// Rows of codes in place: one wave per block of destinations, most of which have few holes or none.  In these moments the block that holds slot
+// `keep` may be getting another exponent; rows that come from it take the one that the plan saw.
+template <int D, typename F>
+__global__ __launch_bounds__(NT) void fill_holes_kernel(MoveArgs a)
+{
+    constexpr int PER_ROW = D / 16, AT_ONCE = 64 / (2 * PER_ROW);      // lanes of a row of one tensor; holes of a round
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int bh = blockIdx.y, b = bh / a.H, h = bh % a.H, blk = blockIdx.x * (NT / 64) + wave, base = blk * CACHE_BLOCK;
+    if (blk >= a.plan.blocks) return;
+    const int *hdr = a.ws + (size_t)bh * a.plan.words, *src = hdr + PLAN_HDR, *dst = src + a.plan.most, *hole_of = dst + a.plan.most;
+    const int i0 = __builtin_amdgcn_readfirstlane(hole_of[blk]), count = __builtin_amdgcn_readfirstlane(hole_of[blk + 1]) - i0;
+    if (count <= 0) return;
+    const int mine = i0 + min(lane, count - 1), from = src[mine], to = dst[mine];         // of hole `lane`
+    const size_t exps = (size_t)bh * cache_blocks(a.L_max);
+    const int tensor = lane / (32), hole = lane % 32 / PER_ROW, part = lane % PER_ROW;
+    const llla_strides &s = tensor ? a.sv : a.sk;
+    int8_t *X = static_cast<int8_t *>(tensor ? a.Vd : a.Kd) + b * s.batch + h * s.head;
+    const int8_t *exp = tensor ? a.ve : a.ke;
+    const int was = exp[exps + blk];
+    int need = EXP_LEAST;
+    for (int i = 0; i < count; i += AT_ONCE) {
+        const int f = __shfl(from, min(i + hole, count - 1)), fb = f / CACHE_BLOCK;
+        const uint4 w = *reinterpret_cast<const uint4 *>(X + (int64_t)f * s.seq + 16 * part);
+        const int e = fb == a.keep / CACHE_BLOCK ? hdr[1 + tensor] : (int)exp[exps + fb];
+        need = exponent_join(need, exponent_needed<F>(w, e));
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) need = exponent_join(need, __shfl_xor(need, off));      // over the 32 lanes of a tensor
+    const int now = exponent_join(was, need);
+    if (now != was && now != EXP_NAN)                     // (rare) the rows that are there
+        for (int r = hole; r < CACHE_BLOCK; r += AT_ONCE)
+            if (base + r < a.keep) {
+                uint4 *p = reinterpret_cast<uint4 *>(X + (int64_t)(base + r) * s.seq + 16 * part);
+                *p = shift16<F>(*p, was, now);
+            }
+    for (int i = 0; i < count; i += AT_ONCE) {
+        const int f = __shfl(from, min(i + hole, count - 1)), t = __shfl(to, min(i + hole, count - 1)), fb = f / CACHE_BLOCK;
+        const uint4 w = *reinterpret_cast<const uint4 *>(X + (int64_t)f * s.seq + 16 * part);
+        const int e = fb == a.keep / CACHE_BLOCK ? hdr[1 + tensor] : (int)exp[exps + fb];
+        if (i + hole < count)
+            *reinterpret_cast<uint4 *>(X + (int64_t)t * s.seq + 16 * part) = now == EXP_NAN || now == e ? w : shift16<F>(w, e, now);
+    }
+    if (lane % 32 == 0) (tensor ? a.ved : a.ked)[exps + blk] = (int8_t)now;
+    if (lane < count) move_row_words(a, bh, from, to);
 }
 
 template <int D>
@@ -593,8 +845,12 @@ hipError_t launch_moves(const EvictProblem &p, MoveArgs a)
 {
     const int bh = p.c.B * p.c.H, size = p.c.type == LLLA_F32 ? 4 : p.c.type == LLLA_BF16 ? 2 : 1;
     if (size == 1) {
-        const dim3 grid(cache_blocks(p.keep), bh);
-        if (p.c.type == LLLA_I8) hipLaunchKernelGGL((move_codes_kernel<D, Int8Code>), grid, dim3(NT), 0, p.stream, a);
+        const int blocks = cache_blocks(p.keep);
+        const dim3 grid(p.in_place ? (blocks + NT / 64 - 1) / (NT / 64) : blocks, bh);
+        const bool i8 = p.c.type == LLLA_I8;
+        if (p.in_place && i8) hipLaunchKernelGGL((fill_holes_kernel<D, Int8Code>), grid, dim3(NT), 0, p.stream, a);
+        else if (p.in_place) hipLaunchKernelGGL((fill_holes_kernel<D, E4m3Code>), grid, dim3(NT), 0, p.stream, a);
+        else if (i8) hipLaunchKernelGGL((move_codes_kernel<D, Int8Code>), grid, dim3(NT), 0, p.stream, a);
         else hipLaunchKernelGGL((move_codes_kernel<D, E4m3Code>), grid, dim3(NT), 0, p.stream, a);
     } else {
         for (llla_strides *s : {&a.sk, &a.sv, &a.dk, &a.dv}) { s->batch *= size; s->head *= size; s->seq *= size; }
@@ -635,9 +891,11 @@ hipError_t cache_evict(const EvictProblem &p)
                       p.keep, p.sinks, p.recent, p.in_place ? 1 : 0, p.lens, p.index, plan, static_cast<int *>(p.ws)};
     const dim3 grid(bh);
     if (c.L_max <= 1024) hipLaunchKernelGGL((evict_plan_kernel<256, 4>), grid, dim3(256), 0, p.stream, a);
-    else if (c.L_max <= 4096) hipLaunchKernelGGL((evict_plan_kernel<256, 16>), grid, dim3(256), 0, p.stream, a);
-    else if (c.L_max <= 16384) hipLaunchKernelGGL((evict_plan_kernel<1024, 16>), grid, dim3(1024), 0, p.stream, a);
-    else hipLaunchKernelGGL((evict_plan_kernel<1024, 0>), grid, dim3(1024), 0, p.stream, a);
+    else if (c.L_max <= 4096) hipLaunchKernelGGL((evict_plan_kernel<1024, 4>), grid, dim3(1024), 0, p.stream, a);
+    else if (c.L_max <= 8192) hipLaunchKernelGGL((evict_plan_kernel<1024, 8>), grid, dim3(1024), 0, p.stream, a);
+    else if (c.L_max <= ONE_LAUNCH) hipLaunchKernelGGL((evict_plan_kernel<1024, 16>), grid, dim3(1024), 0, p.stream, a);
+    else
+        for (int step = 0; step <= 5; ++step) hipLaunchKernelGGL(evict_long_kernel, dim3(plan.chunks, bh), dim3(NT), 0, p.stream, a, step);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || plan.most == 0) return e;
     const MoveArgs m{c.K, c.V, d.K, d.V, c.sk, c.sv, d.sk, d.sv, c.k_exp, c.v_exp, d.k_exp, d.v_exp, c.scores, c.pos, d.scores, d.pos,
