@@ -1,20 +1,21 @@
-// Decode over an 8-bit cache: one pass over the cache, the method of llla_mfma_decode_f32.hip (its layout of rows in lanes, reference exponent,
-// records, merge and solve), with operands made for codes.
+// Decode over an 8-bit cache: one pass over the cache, the method of llla_mfma_decode.hip (moments relative to a reference exponent,
+// records, merge and solve), with operands made of codes.
 //
 // A code times a power of two is an f16 number, so keys and values are operands of 16-bit matrix instructions as they are; only the
-// weighted key x = w k needs more bits and is taken in two f16 terms, x = h + l with l = x - h rounded (22 bits and the sign of l).  The second
-// moment sum w k k^T and sum w k v^T then cost two products per tile, against six for fp32 rows, and carry the precision of fp32.
-// f16 has few exponents, so everything is relative:  k16 = k 2^-(E + U), E the largest exponent of the blocks that the wave reads and U
-// the format's unit (int8 codes land in +-1/4, e4m3 ones in +-57344); weights are relative to 2^R, R following the largest logit such that
-// |w k16| stays below 2^16.  The least number of f16, 2^-24, is then 2^-38 of the largest x, and a block's codes are exact as long as its
-// exponent is at most 15 (int8) or 22 (e4m3) below E.
+// weighted key x = w k is rounded.  Two variants, chosen per sequence:
+//   two terms: x = h + l, l = x - h rounded (22 bits and the sign of l), weights in fp32.  The products of 32 keys start from zero and are then
+//              added, one rounding of the sum for them: the precision of fp32 (which six products per tile give for fp32 rows).  For fp32 results,
+//              and for sequences of at most 4 d keys, where only the ridge holds some directions and rounding x to 11 bits is not small against it.
+//   one term:  w rounded to f16, and that same number used in every moment; x = w k rounded to f16.  2.5e-4 of the result, a seventh of the rounding of
+//              a bf16 result.
+// f16 has few exponents, so everything is relative: operands are k 2^-(E + U), E the largest exponent of the blocks that the wave reads and U the format's
+// unit, which puts the largest code at 1/4; weights are relative to 2^R, R following the largest logit such that |w k| stays below 2^16.  The
+// least number of f16, 2^-24, is then 2^-37 of the largest x and 2^-22 of the largest key.
 //
-// Lane (g, n) owns features NB n .. NB n + NB - 1 (NB = d / 16) of key g of a chunk of four: NB bytes.  Two chunks' words give the pairs of an
-// operand: int8 bytes of both, each in the low half of a 16-bit field, are f16 numbers u 2^-24 (subnormal, u = code + 128), which one
-// packed multiply-add turns into (u - 128) 2^-9 r, r the block's power relative to E; e4m3 has a conversion with a scale.
-//
-// A step is 32 keys of one block.  At d = 128 the four waves of a workgroup share a key stream and the row blocks of the moments (W and 7 - W
-// each), and every wave forms the operands for itself.
+// Rows come by DMA into LDS, a block of 64 keys (one exponent) per stage, in 16-byte chunks whose order is permuted so that the transposed reads
+// (ds_read_b64_tr_b8: eight keys of one feature per lane, which is an operand's order) have no bank conflicts.  int8: the low halves of 16-bit fields
+// are f16 numbers u 2^-24 (subnormal, u = code + 128), which one packed multiply-add turns into (u - 128) 2^-9 r, r the block's power relative
+// to E; e4m3 has a conversion with a scale.
 #include "llla_cache.hpp"
 #include "llla_decode_tail.hpp"
 
@@ -39,82 +40,71 @@ namespace {
 
 using namespace mfma;
 
-constexpr int NT = DEC_NT, STEP = 32, CH = 8;
+constexpr int NT = DEC_NT, KEYS = CACHE_BLOCK;            // keys of a stage
 
 template <int D>
 struct Q8Shape : DecShape<D> {
-    static constexpr bool TEAM = D == 128;
+    static constexpr bool TEAM = D == 128;                // four waves share one key stream
     static constexpr int NR = TEAM ? 2 : D / 16;          // row blocks of a wave
     static constexpr int NBUF = D <= 32 ? 4 : TEAM ? 1 : 2;
-    static constexpr int WORDS = D == 128 ? 2 : 1;        // words of a row that a lane owns
     static constexpr int KEYS_MIN = TEAM ? 256 : 512;     // fewest keys worth a workgroup
     static constexpr int SLOTS = 512;                     // workgroups worth having at once
     static constexpr int MAX_SPLIT = 32;
+    static constexpr int CPR = D / 16;                    // 16-byte chunks of a row
+    static constexpr int TILE_B = KEYS * D;               // keys or values of a stage
+    static constexpr int DMAS = TILE_B / 1024;            // transfers of a tile
+    static constexpr int STAGES = 2;
 };
 
-// value = operand * 2^(E + UNIT); weights reach 2^(TOP + 2), an operand times a weight 2^16
+// value = operand * 2^(E + UNIT); weights of one term are f16 numbers, of two terms reach 2^17
 template <typename F> struct Unit;
-template <> struct Unit<Int8Code> { static constexpr int EXP = 9, TOP = 15; };
-template <> struct Unit<E4m3Code> { static constexpr int EXP = -7, TOP = -2; };
+template <> struct Unit<Int8Code> { static constexpr int EXP = 9; };
+template <> struct Unit<E4m3Code> { static constexpr int EXP = 11; };
+constexpr int SLACK = 2;                                  // the reference moves when a logit exceeds what it was made for by more than this
+template <bool TWO> constexpr int TOP = TWO ? 15 : 13;    // the largest weight when it moves
 
 typedef _Float16 half2q __attribute__((ext_vector_type(2)));
+typedef int int2q __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) int2q *lds_int2;
 
-template <int WORDS> struct Codes { unsigned u[WORDS]; };
-
-template <int NB>
-__device__ __forceinline__ Codes<(NB > 4 ? 2 : 1)> load_codes(const char *p)
+// eight codes (eight keys of a feature) as an operand; r, z: the block's power relative to E, for int8 as the factor and the addend of u 2^-24
+struct BlockPower { float r; half2q s, z; };
+template <typename F>
+__device__ __forceinline__ BlockPower block_power(int below)
 {
-    Codes<(NB > 4 ? 2 : 1)> c;
-    if constexpr (NB == 1) c.u[0] = *reinterpret_cast<const uint8_t *>(p);
-    else if constexpr (NB == 2) c.u[0] = *reinterpret_cast<const uint16_t *>(p);
-    else if constexpr (NB == 4) c.u[0] = __builtin_nontemporal_load(reinterpret_cast<const unsigned *>(p));
-    else {
-        const uint2 v = *reinterpret_cast<const uint2 *>(p);
-        c.u[0] = v.x; c.u[1] = v.y;
-    }
-    return c;
-}
-
-// Operands of the NB feature blocks from the words of eight chunks; `below`: how far the block's exponent is below E
-template <int NB, typename F, int WORDS>
-__device__ __forceinline__ void make_operands(half8 (&o)[NB], const Codes<WORDS> (&c)[CH], int below)
-{
+    BlockPower b;
     if constexpr (std::is_same<F, Int8Code>::value) {
-        const float r = __builtin_ldexpf(1.f, -below);
-        const _Float16 s = (_Float16)(r * 32768.f), z = (_Float16)(r * -0.25f);
-        const half2q s2 = {s, s}, z2 = {z, z};
-        unsigned u[CH][WORDS];
-#pragma unroll
-        for (int t = 0; t < CH; ++t)
-#pragma unroll
-            for (int w = 0; w < WORDS; ++w) u[t][w] = c[t].u[w] ^ 0x80808080u;
-#pragma unroll
-        for (int i = 0; i < NB; ++i)
-#pragma unroll
-            for (int t = 0; t < CH; t += 2) {
-                const unsigned sel = 0x0c000c00u | ((unsigned)(4 + i % 4) << 16) | (unsigned)(i % 4);
-                const half2q v = __builtin_elementwise_fma(__builtin_bit_cast(half2q, __builtin_amdgcn_perm(u[t + 1][i / 4], u[t][i / 4], sel)), s2, z2);
-                o[i][t] = v[0];
-                o[i][t + 1] = v[1];
-            }
+        b.r = __builtin_ldexpf(1.f, -below);
+        const _Float16 s = (_Float16)(b.r * 32768.f), z = (_Float16)(b.r * -0.25f);
+        b.s = half2q{s, s};
+        b.z = half2q{z, z};
     } else {
-        const float scale = __builtin_ldexpf(1.f, 7 - below);
-#pragma unroll
-        for (int t = 0; t < CH; t += 2)
-#pragma unroll
-            for (int i = 0; i < NB; i += 2) {             // bytes of features i and i + 1 of both chunks
-                const unsigned lo = i % 4, sel = lo | ((4 + lo) << 8) | ((lo + 1) << 16) | ((5 + lo) << 24);
-                const unsigned w = __builtin_amdgcn_perm(c[t + 1].u[i / 4], c[t].u[i / 4], sel);
-                const half2q a = __builtin_bit_cast(half2q, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, false));
-                o[i][t] = a[0];
-                o[i][t + 1] = a[1];
-                if (i + 1 < NB) {
-                    const half2q b = __builtin_bit_cast(half2q, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, true));
-                    o[i + 1][t] = b[0];
-                    o[i + 1][t + 1] = b[1];
-                }
-            }
+        b.r = __builtin_ldexpf(1.f, -11 - below);
+        b.s = b.z = half2q{0, 0};
     }
+    return b;
+}
+template <typename F>
+__device__ __forceinline__ half8 operand(int2q c, const BlockPower &b)
+{
+    half8 o;
+    if constexpr (std::is_same<F, Int8Code>::value) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const unsigned u = (unsigned)c[i] ^ 0x80808080u;
+            const half2q lo = __builtin_elementwise_fma(__builtin_bit_cast(half2q, __builtin_amdgcn_perm(0u, u, 0x0c010c00u)), b.s, b.z);
+            const half2q hi = __builtin_elementwise_fma(__builtin_bit_cast(half2q, __builtin_amdgcn_perm(0u, u, 0x0c030c02u)), b.s, b.z);
+            o[4 * i] = lo[0]; o[4 * i + 1] = lo[1]; o[4 * i + 2] = hi[0]; o[4 * i + 3] = hi[1];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const half2q lo = __builtin_bit_cast(half2q, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((unsigned)c[i], b.r, false));
+            const half2q hi = __builtin_bit_cast(half2q, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((unsigned)c[i], b.r, true));
+            o[4 * i] = lo[0]; o[4 * i + 1] = lo[1]; o[4 * i + 2] = hi[0]; o[4 * i + 3] = hi[1];
+        }
+    }
+    return o;
 }
 
 // sums of p[0..3] over the 16 lanes of a row; lane n receives the sum of p[n & 3]
@@ -129,6 +119,22 @@ __device__ __forceinline__ float reduce4(const float *p, int nn)
     return s;
 }
 
+// sum of a[0..7] b[0..7] onto c (v_dot2_f32_f16: exact products)
+__device__ __forceinline__ float dot8(half8 a, half8 b, float c)
+{
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+        c = __builtin_amdgcn_fdot2(h2{a[i], a[i + 1]}, h2{b[i], b[i + 1]}, c, false);
+    }
+    return c;
+}
+
+// The value from here on is another one to the compiler: neither what was computed from it is kept for later, nor is a sum put off with its terms kept
+__device__ __forceinline__ void pin(half8 &x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void pin(f32x4 &x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void pin(float &x) { asm volatile("" : "+v"(x)); }
+
 struct Q8Args {
     const char *K, *V;
     llla_strides sk, sv;
@@ -140,47 +146,265 @@ struct Q8Args {
     float *parts;
 };
 
-template <int D, typename F, typename TQ, bool FUSED, int W, class Lds>
-__device__ __forceinline__ void decode_q8_body(const Q8Args &a, const DecPiece &pc, Lds &lds, int wave, int lane)
+template <int N>
+__device__ __forceinline__ void wait_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// One wave's share of a piece, d <= 64
+template <int D, typename F, typename TQ, bool FUSED, bool TWO, class Lds>
+__device__ __forceinline__ void decode_q8_body(const Q8Args &a, const DecPiece &pc, Lds &lds, unsigned char *stages, int wave, int lane)
 {
     using S = Q8Shape<D>;
-    using U = Unit<F>;
-    constexpr int NB = S::NB, NR = S::NR;
-    constexpr int row[4] = {S::TEAM ? W : 0, S::TEAM ? 7 - W : 1, 2, 3};
+    constexpr int NB = S::NB, U = Unit<F>::EXP, CPR = S::CPR, DMAS = S::DMAS;
     const int g = lane / 16, nn = lane % 16;
     const int L = pc.L, b = pc.b, bh = pc.bh, hc = pc.h / a.group;
-    // pieces begin at blocks of the format, and so do no two waves read one step
-    const int p0 = min((pc.k0 + CACHE_BLOCK - 1) & ~(CACHE_BLOCK - 1), L), p1 = pc.k1 >= L ? L : min((pc.k1 + CACHE_BLOCK - 1) & ~(CACHE_BLOCK - 1), L);
-    const int share = S::TEAM ? p1 - p0 : ((p1 - p0 + 3) / 4 + STEP - 1) / STEP * STEP;
-    const int r0 = __builtin_amdgcn_readfirstlane(min(p0 + (S::TEAM ? 0 : wave * share), p1));
+    // shares begin at blocks of the format
+    const int p0 = min((pc.k0 + KEYS - 1) & ~(KEYS - 1), L), p1 = pc.k1 >= L ? L : min((pc.k1 + KEYS - 1) & ~(KEYS - 1), L);
+    const int share = ((p1 - p0 + 3) / 4 + KEYS - 1) / KEYS * KEYS;
+    const int r0 = __builtin_amdgcn_readfirstlane(min(p0 + wave * share, p1));
     const int r1 = __builtin_amdgcn_readfirstlane(min(r0 + share, p1));
-    const int nsteps = (r1 - r0 + STEP - 1) / STEP;
+    const int nsteps = (r1 - r0 + KEYS - 1) / KEYS, b0 = r0 / KEYS;
     const char *Kh = a.K + b * a.sk.batch + hc * a.sk.head, *Vh = a.V + b * a.sv.batch + hc * a.sv.head;
     const int64_t krow = a.sk.seq, vrow = a.sv.seq;
-    const unsigned koff = (unsigned)(g * (int)krow + NB * nn), voff = (unsigned)(g * (int)vrow + NB * nn);
-    const int8_t *ke = a.ke + (size_t)(b * a.HC + hc) * a.blocks, *ve = a.ve + (size_t)(b * a.HC + hc) * a.blocks;
+    const int8_t *ke = a.ke + (size_t)(b * a.HC + hc) * a.blocks + b0, *ve = a.ve + (size_t)(b * a.HC + hc) * a.blocks + b0;
 
-    struct Step { Codes<S::WORDS> k[CH], v[CH]; };
-    auto load = [&](Step &st, int s) {
-        const int j0 = r0 + (s < nsteps ? s : 0) * STEP;  // past the end: the first step again, never used
-        if (j0 + STEP <= L) {
+    f32x4 acc[S::NTILES];
+    float mu[NB], yv[NB], q[NB];
+#pragma unroll
+    for (int t = 0; t < S::NTILES; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NB; ++i) { mu[i] = 0.f; yv[i] = 0.f; }
+    float om = 0.f, mref = -INFINITY, mtrue = -INFINITY;
+    int EK = EXP_NAN, EV = EXP_NAN;                       // largest exponents of the blocks read
+
+    // Transfers: lane l brings chunk position l % CPR of key l / CPR of a group of 64 / CPR keys; the chunk of a row that lies at position p is
+    // p ^ turn(key), turn the same for the same lane in every group.
+    constexpr int KPD = 64 / CPR;
+    const int dkey = lane / CPR, dchunk = (lane % CPR) ^ (D == 64 ? lane / 16 : D == 32 ? (lane / 16) & 1 : 0);
+    unsigned char *const mine = stages + wave * (2 * S::STAGES * S::TILE_B);
+    const unsigned mine_off = lds_offset(mine);
+    const unsigned koff = (unsigned)(dkey * (int)krow + 16 * dchunk), voff = (unsigned)(dkey * (int)vrow + 16 * dchunk);
+    // Waves that start together on equally spaced addresses would keep hitting the same memory channels in step: each begins at another block
+    // of its share and wraps around.
+    const int rot = nsteps > 0 ? __builtin_amdgcn_readfirstlane((int)(((unsigned)pc.rec * 4u + wave) * 7u % (unsigned)nsteps)) : 0;
+    auto block_of = [&](int s) { const int t = s + rot; return t >= nsteps ? t - nsteps : t; };
+    auto fetch = [&](int s, int stage) {
+        const int j0 = r0 + block_of(s) * KEYS;
+        const unsigned dst = mine_off + (unsigned)(stage * 2 * S::TILE_B);
+        if (j0 + KEYS <= L) {
             const char *kp = Kh + j0 * krow, *vp = Vh + j0 * vrow;
 #pragma unroll
-            for (int c = 0; c < CH; ++c) st.k[c] = load_codes<NB>(kp + 4 * c * krow + koff);
+            for (int t = 0; t < DMAS; ++t) dma16_base_nt_off(kp + t * KPD * krow, koff, dst + 1024u * t);
 #pragma unroll
-            for (int c = 0; c < CH; ++c) st.v[c] = load_codes<NB>(vp + 4 * c * vrow + voff);
+            for (int t = 0; t < DMAS; ++t) dma16_base_nt_off(vp + t * KPD * vrow, voff, dst + S::TILE_B + 1024u * t);
         } else {                                          // rows beyond the sequence: its last row (their weights are 0)
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const int64_t j = min(j0 + 4 * c + g, L - 1);
-                st.k[c] = load_codes<NB>(Kh + j * krow + NB * nn);
-                st.v[c] = load_codes<NB>(Vh + j * vrow + NB * nn);
-            }
+            for (int t = 0; t < DMAS; ++t) dma16_nt_off(Kh + min(j0 + t * KPD + dkey, L - 1) * krow + 16 * dchunk, dst + 1024u * t);
+#pragma unroll
+            for (int t = 0; t < DMAS; ++t) dma16_nt_off(Vh + min(j0 + t * KPD + dkey, L - 1) * vrow + 16 * dchunk, dst + S::TILE_B + 1024u * t);
         }
     };
+    // transposed reads: lane (g, j) addresses eight bytes of key 8 g + j / 2 and receives eight keys of feature 16 I + j
+    const int tkey = 8 * g + nn / 2, turn = D == 64 ? (tkey >> 2) & 3 : D == 32 ? (tkey >> 3) & 1 : 0;
+    auto read = [&](int stage, int tile, int half, int I) {
+        const unsigned at = (unsigned)(tkey * D + 16 * (I ^ turn) + 8 * (nn & 1));
+        const unsigned char *p = mine + stage * 2 * S::TILE_B + tile * S::TILE_B + half * 32 * D;
+        return __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_int2)(lds_void_ptr)(p + at));
+    };
 
-    f32x4 acc[S::NTILES];                                 // (TEAM: the tiles of row blocks row[0] and row[1] only)
-    float mu[NR], yv[NR], q[NB];
+    if (nsteps > 0) {
+        fetch(0, 0);
+        if (nsteps > 1) fetch(1, 1);
+        {
+            const TQ *qp = static_cast<const TQ *>(a.out.q) + (size_t)bh * D + nn;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                if constexpr (sizeof(TQ) == 2) q[i] = bf16_to_f32(qp[16 * i]) * a.cscale;
+                else q[i] = qp[16 * i] * a.cscale;
+            }
+        }
+        for (int i = lane; i < nsteps; i += 64) {
+            EK = max(EK, (int)ke[i]);
+            EV = max(EV, (int)ve[i]);
+        }
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) {
+            EK = max(EK, __shfl_xor(EK, off));
+            EV = max(EV, __shfl_xor(EV, off));
+        }
+        EK = __builtin_amdgcn_readfirstlane(EK);
+        EV = __builtin_amdgcn_readfirstlane(EV);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) q[i] = __builtin_ldexpf(q[i], EK + U);
+
+        int ek64 = 0, ev64 = 0, have = -1;                // exponents of 64 blocks, one per lane; which 64
+        auto compute = [&](int s, auto stage_tag) {
+            constexpr int stage = decltype(stage_tag)::value;
+            const int blk = block_of(s), j0 = r0 + blk * KEYS;
+            if (blk / 64 != have) {
+                have = blk / 64;
+                const int i = min(64 * have + lane, nsteps - 1);
+                ek64 = ke[i];
+                ev64 = ve[i];
+            }
+            const int e_k = __builtin_amdgcn_readlane(ek64, blk % 64), e_v = __builtin_amdgcn_readlane(ev64, blk % 64);
+            const BlockPower pk = block_power<F>(EK - e_k), pv = block_power<F>(EV - e_v);
+            if (s + 1 < nsteps) wait_but<2 * DMAS>();
+            else wait_but<0>();
+            half8 k[2][NB];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int I = 0; I < NB; ++I) k[h][I] = operand<F>(read(stage, 0, h, I), pk);
+            float t[4];                                   // logit (log2 units) of key 32 h + 8 g + 4 c + (n % 4) in t[2 h + c]
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float p[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[e] = 0.f;
+#pragma unroll
+                        for (int I = 0; I < NB; ++I) p[e] = fmaf((float)k[h][I][4 * c + e], q[I], p[e]);
+                    }
+                    t[2 * h + c] = reduce4(p, nn);
+                }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int I = 0; I < NB; ++I) pin(k[h][I]);
+            if (e_k == EXP_NAN || e_v == EXP_NAN) t[0] = t[1] = t[2] = t[3] = NAN;      // (a scalar branch)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t[i] = j0 + 32 * (i / 2) + 8 * g + 4 * (i % 2) + (nn & 3) < r1 ? t[i] : -INFINITY;
+            const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+            if (__builtin_amdgcn_ballot_w64(top > mref + (TOP<TWO> + SLACK)) != 0) {
+                const float mnew = wave_max_dpp(top) - TOP<TWO>;
+                const float alpha = mref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mref - mnew);
+                mref = mnew;
+                om *= alpha;
+#pragma unroll
+                for (int i = 0; i < NB; ++i) { mu[i] *= alpha; yv[i] *= alpha; }
+#pragma unroll
+                for (int i = 0; i < S::NTILES; ++i) acc[i] *= alpha;
+            }
+            mtrue = fmaxf(mtrue, top);
+            float w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = __builtin_amdgcn_exp2f(t[i] - mref);           // exp2(-inf) = 0 masks the tail
+                if constexpr (!TWO) w[i] = (float)(_Float16)w[i];
+                om += w[i];
+            }
+            auto spread = [&](int h, float (&o)[8]) {                 // the weights of a half's keys in the operands' order
+                o[0] = row_bcast<0>(w[2 * h]); o[1] = row_bcast<1>(w[2 * h]); o[2] = row_bcast<2>(w[2 * h]); o[3] = row_bcast<3>(w[2 * h]);
+                o[4] = row_bcast<0>(w[2 * h + 1]); o[5] = row_bcast<1>(w[2 * h + 1]); o[6] = row_bcast<2>(w[2 * h + 1]); o[7] = row_bcast<3>(w[2 * h + 1]);
+            };
+            // (the scheduler is kept inside one block of features: left to itself it reads and converts the whole stage first and spills)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float wc[8];
+                spread(h, wc);
+                half8 w8, x[NB], xl[NB];                  // (w8 with one term, xl with two)
+                if constexpr (!TWO) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) w8[c] = (_Float16)wc[c];
+                }
+                auto product = [&](int I, const half8 &b, f32x4 &sum) {
+                    if constexpr (!TWO) sum = mfma_f16(x[I], b, sum);
+                    else sum += mfma_f16(x[I], b, mfma_f16(xl[I], b, f32x4{0.f, 0.f, 0.f, 0.f}));
+                };
+#pragma unroll
+                for (int J = 0; J < NB; ++J) {
+                    if constexpr (!TWO) {
+                        x[J] = w8 * k[h][J];
+                        mu[J] = dot8(w8, k[h][J], mu[J]);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            const float kf = (float)k[h][J][c];
+                            x[J][c] = (_Float16)(wc[c] * kf);
+                            xl[J][c] = (_Float16)fmaf(wc[c], kf, -(float)x[J][c]);
+                            mu[J] = fmaf(wc[c], kf, mu[J]);
+                        }
+                    }
+#pragma unroll
+                    for (int I = 0; I <= J; ++I) product(I, k[h][J], acc[upper_tile<NB>(I, J)]);
+                    pin(mu[J]);
+                    pin(x[J]);
+                    if constexpr (TWO) pin(xl[J]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int J = 0; J < NB; ++J) {
+                    const half8 v = operand<F>(read(stage, 1, h, J), pv);
+                    if constexpr (!TWO) yv[J] = dot8(w8, v, yv[J]);
+                    else {
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) yv[J] = fmaf(wc[c], (float)v[c], yv[J]);
+                    }
+#pragma unroll
+                    for (int I = 0; I < NB; ++I) product(I, v, acc[S::NSIG + NB * I + J]);
+                    pin(yv[J]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // read before the transfer that overwrites them is requested
+            if (s + 2 < nsteps) fetch(s + 2, stage);
+        };
+#pragma unroll 1
+        for (int s = 0; s < nsteps; s += 2) {
+            compute(s, std::integral_constant<int, 0>{});
+            if (s + 1 < nsteps) compute(s + 1, std::integral_constant<int, 1>{});
+        }
+        // back from the operands' scale
+#pragma unroll
+        for (int t = 0; t < S::NTILES; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[t][i] = __builtin_ldexpf(acc[t][i], EK + U + (t < S::NSIG ? EK : EV) + U);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            mu[i] = __builtin_ldexpf(mu[i], EK + U);
+            yv[i] = __builtin_ldexpf(yv[i], EV + U);
+        }
+    }
+
+    __syncthreads();                                      // the stages of all waves are dead: the merge takes their place
+    mtrue = wave_max_dpp(mtrue);
+    om += dpp_f<0xB1>(om);
+    om += dpp_f<0x4E>(om);
+    om = rows_allsum(om);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) { mu[i] = rows_allsum(mu[i]); yv[i] = rows_allsum(yv[i]); }
+    float *R = a.parts + (size_t)pc.rec * S::REC_F;       // this workgroup's record (not FUSED)
+    finish_workgroup<D, TQ, false, FUSED, S::NBUF>(lds, acc, mu, yv, om, mref, mtrue, R, a.out, bh, wave, lane);
+}
+
+// d = 128: the four waves of a workgroup share a key stream.  Wave W owns row blocks W and 7 - W of the moments (25 tiles whatever W) and forms of the
+// keys and values what it multiplies with; logits it sums over its own two feature blocks, one stage ahead, and the four partial sums meet in LDS.  One
+// barrier per stage: behind it the next stage's rows are there, this stage's partial logits are, and the stage before last is free for a transfer.
+constexpr int WIDE_STAGES = 4, WIDE_STAGE_B = 2 * KEYS * 128;
+struct WideLds {
+    unsigned char rows[WIDE_STAGES][WIDE_STAGE_B];
+    float part[2][KEYS][4];
+};
+
+template <typename F, typename TQ, bool FUSED, bool TWO, int W, class Lds>
+__device__ __forceinline__ void decode_q8_wide_body(const Q8Args &a, const DecPiece &pc, Lds &lds, WideLds &wl, int wave, int lane)
+{
+    constexpr int D = 128, NB = 8, NR = 2, U = Unit<F>::EXP;
+    using S = Q8Shape<D>;
+    constexpr int row[NR] = {W, 7 - W}, low = W < 4 ? W : 7 - W;
+    const int g = lane / 16, nn = lane % 16;
+    const int L = pc.L, b = pc.b, bh = pc.bh, hc = pc.h / a.group;
+    const int r0 = __builtin_amdgcn_readfirstlane(min((pc.k0 + KEYS - 1) & ~(KEYS - 1), L));
+    const int r1 = __builtin_amdgcn_readfirstlane(pc.k1 >= L ? L : min((pc.k1 + KEYS - 1) & ~(KEYS - 1), L));
+    const int nsteps = (r1 - r0 + KEYS - 1) / KEYS, b0 = r0 / KEYS;
+    const char *Kh = a.K + b * a.sk.batch + hc * a.sk.head, *Vh = a.V + b * a.sv.batch + hc * a.sv.head;
+    const int64_t krow = a.sk.seq, vrow = a.sv.seq;
+    const int8_t *ke = a.ke + (size_t)(b * a.HC + hc) * a.blocks + b0, *ve = a.ve + (size_t)(b * a.HC + hc) * a.blocks + b0;
+
+    f32x4 acc[S::NTILES];                                 // the tiles of row blocks row[0] and row[1] only
+    float mu[NR], yv[NR], q[NR];
 #pragma unroll
     for (int t = 0; t < S::NTILES; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -195,20 +419,49 @@ __device__ __forceinline__ void decode_q8_body(const Q8Args &a, const DecPiece &
         }
     };
     float om = 0.f, mref = -INFINITY, mtrue = -INFINITY;
-    int EK = EXP_NAN, EV = EXP_NAN;                       // largest exponents of the blocks read
-    if (nsteps > 0) {
-        Step sa, sb;
-        load(sa, 0);
-        {
-            const TQ *qp = static_cast<const TQ *>(a.out.q) + (size_t)bh * D + NB * nn;
+    int EK = EXP_NAN, EV = EXP_NAN;
+
+    // transfers: of the eight of a tile (eight keys each) wave W brings numbers 2 W and 2 W + 1
+    const int dkey = lane / 8, dchunk = (lane % 8) ^ (lane / 16);
+    const unsigned koff = (unsigned)(dkey * (int)krow + 16 * dchunk), voff = (unsigned)(dkey * (int)vrow + 16 * dchunk);
+    const unsigned rows_off = lds_offset(wl.rows);
+    const int rot = nsteps > 0 ? __builtin_amdgcn_readfirstlane((int)((unsigned)pc.rec * 7u % (unsigned)nsteps)) : 0;
+    auto block_of = [&](int s) { const int t = s + rot; return t >= nsteps ? t - nsteps : t; };
+    auto fetch = [&](int s) {
+        const int j0 = r0 + block_of(s) * KEYS;
+        const unsigned dst = rows_off + (unsigned)((s & (WIDE_STAGES - 1)) * WIDE_STAGE_B);
 #pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                if constexpr (sizeof(TQ) == 2) q[i] = bf16_to_f32(qp[i]) * a.cscale;
-                else q[i] = qp[i] * a.cscale;
+        for (int tile = 0; tile < 2; ++tile) {
+            const char *X = tile ? Vh : Kh;
+            const int64_t pitch = tile ? vrow : krow;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int t = 2 * W + i;
+                const unsigned to = dst + (unsigned)(tile * KEYS * D + 1024 * t), turn = 64u * i;      // (odd groups: the other half of the chunks)
+                if (j0 + KEYS <= L) dma16_base_nt_off(X + (j0 + 8 * t) * pitch, (tile ? voff : koff) ^ turn, to);
+                else dma16_nt_off(X + min(j0 + 8 * t + dkey, L - 1) * pitch + (16 * dchunk ^ turn), to);
             }
         }
-        const int b0 = r0 / CACHE_BLOCK, b1 = (r1 - 1) / CACHE_BLOCK;
-        for (int i = b0 + lane; i <= b1; i += 64) {
+    };
+    const int tkey = 8 * g + nn / 2, turn = 4 * (g & 1) + (nn >> 2);
+    auto read = [&](int s, int tile, int half, int I) {
+        const unsigned at = (unsigned)((32 * half + tkey) * D + 16 * (I ^ turn) + 8 * (nn & 1));
+        return __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_int2)(lds_void_ptr)(wl.rows[s & (WIDE_STAGES - 1)] + tile * KEYS * D + at));
+    };
+
+    if (nsteps > 0) {
+        fetch(0);
+        if (nsteps > 1) fetch(1);
+        if (nsteps > 2) fetch(2);
+        {
+            const TQ *qp = static_cast<const TQ *>(a.out.q) + (size_t)bh * D + nn;
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                if constexpr (sizeof(TQ) == 2) q[i] = bf16_to_f32(qp[16 * row[i]]) * a.cscale;
+                else q[i] = qp[16 * row[i]] * a.cscale;
+            }
+        }
+        for (int i = lane; i < nsteps; i += 64) {
             EK = max(EK, (int)ke[i]);
             EV = max(EV, (int)ve[i]);
         }
@@ -220,85 +473,152 @@ __device__ __forceinline__ void decode_q8_body(const Q8Args &a, const DecPiece &
         EK = __builtin_amdgcn_readfirstlane(EK);
         EV = __builtin_amdgcn_readfirstlane(EV);
 #pragma unroll
-        for (int i = 0; i < NB; ++i) q[i] = __builtin_ldexpf(q[i], EK + U::EXP);
+        for (int i = 0; i < NR; ++i) q[i] = __builtin_ldexpf(q[i], EK + U);
 
-        int ek64 = 0, ev64 = 0;                           // exponents of 64 blocks, one per lane
-        auto compute = [&](const Step &st, int s) {
-            const int j0 = r0 + s * STEP, at = j0 / CACHE_BLOCK - b0;
-            if (at % 64 == 0 && (s == 0 || j0 % CACHE_BLOCK == 0)) {
-                const int i = min(b0 + at + lane, b1);
+        int ek64 = 0, ev64 = 0, have = -1;
+        BlockPower pk, pv;
+        bool marked = false;
+        half8 kown[2][NR];
+        auto partial_logits = [&](int s) {                // and the operands of this wave's row blocks
+            const int blk = block_of(s);
+            if (blk / 64 != have) {
+                have = blk / 64;
+                const int i = min(64 * have + lane, nsteps - 1);
                 ek64 = ke[i];
                 ev64 = ve[i];
             }
-            const int e_k = __builtin_amdgcn_readlane(ek64, at % 64), e_v = __builtin_amdgcn_readlane(ev64, at % 64);
-            half8 kh[NB], vh[NB];
-            make_operands<NB, F>(kh, st.k, EK - e_k);
-            float t[2];
+            const int e_k = __builtin_amdgcn_readlane(ek64, blk % 64), e_v = __builtin_amdgcn_readlane(ev64, blk % 64);
+            pk = block_power<F>(EK - e_k);
+            pv = block_power<F>(EV - e_v);
+            marked = e_k == EXP_NAN || e_v == EXP_NAN;
 #pragma unroll
-            for (int grp = 0; grp < 2; ++grp) {
-                float p[4];
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    p[c] = 0.f;
+                for (int i = 0; i < NR; ++i) kown[h][i] = operand<F>(read(s, 0, h, row[i]), pk);
 #pragma unroll
-                    for (int i = 0; i < NB; ++i) p[c] = fmaf((float)kh[i][4 * grp + c], q[i], p[c]);
+                for (int c = 0; c < 2; ++c) {
+                    float p[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[e] = fmaf((float)kown[h][1][4 * c + e], q[1], (float)kown[h][0][4 * c + e] * q[0]);
+                    const float t = reduce4(p, nn);
+                    if (c == 1) { pin(kown[h][0]); pin(kown[h][1]); }
+                    if (nn < 4) wl.part[s & 1][32 * h + 8 * g + 4 * c + nn][W] = t;
                 }
-                t[grp] = reduce4(p, nn);                  // logit (log2 units) of key 4 (n % 4) + g of the group
-                if (e_k == EXP_NAN || e_v == EXP_NAN) t[grp] = NAN;      // (a scalar branch)
-                t[grp] = j0 + grp * 16 + 4 * (nn & 3) + g < r1 ? t[grp] : -INFINITY;
             }
-            const float top = fmaxf(t[0], t[1]);
-            if (__builtin_amdgcn_ballot_w64(top > mref + (U::TOP + 2)) != 0) {
-                const float mnew = wave_max_dpp(top) - U::TOP;
+        };
+        auto meet = [&](bool later) {                     // later: the next stage but one is still on its way
+            if (later) wait_but<4>();
+            else wait_but<0>();
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        };
+        if (nsteps > 2) wait_but<8>();
+        else if (nsteps > 1) wait_but<4>();
+        else wait_but<0>();
+        asm volatile("s_barrier" ::: "memory");
+        partial_logits(0);
+#pragma unroll 1
+        for (int s = 0; s < nsteps; ++s) {
+            meet(s + 2 < nsteps);
+            if (s + 3 < nsteps) fetch(s + 3);
+            const int j0 = r0 + block_of(s) * KEYS;
+            float t[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int key = 32 * (i / 2) + 8 * g + 4 * (i % 2) + (nn & 3);
+                const f32x4 p = *reinterpret_cast<const f32x4 *>(wl.part[s & 1][key]);
+                t[i] = marked ? NAN : (p[0] + p[1]) + (p[2] + p[3]);
+                t[i] = j0 + key < r1 ? t[i] : -INFINITY;
+            }
+            const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+            if (__builtin_amdgcn_ballot_w64(top > mref + (TOP<TWO> + SLACK)) != 0) {
+                const float mnew = wave_max_dpp(top) - TOP<TWO>;
                 const float alpha = mref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mref - mnew);
                 mref = mnew;
                 om *= alpha;
 #pragma unroll
                 for (int i = 0; i < NR; ++i) { mu[i] *= alpha; yv[i] *= alpha; }
-                for_tiles([&](int t, bool) { acc[t] *= alpha; });
+                for_tiles([&](int i, bool) { acc[i] *= alpha; });
             }
             mtrue = fmaxf(mtrue, top);
-            float w[2];
+            float w[4];
 #pragma unroll
-            for (int grp = 0; grp < 2; ++grp) {
-                w[grp] = __builtin_amdgcn_exp2f(t[grp] - mref);       // exp2(-inf) = 0 masks the tail
-                om += w[grp];
+            for (int i = 0; i < 4; ++i) {
+                w[i] = __builtin_amdgcn_exp2f(t[i] - mref);
+                if constexpr (!TWO) w[i] = (float)(_Float16)w[i];
+                om += w[i];
             }
-            const float wc[8] = {row_bcast<0>(w[0]), row_bcast<1>(w[0]), row_bcast<2>(w[0]), row_bcast<3>(w[0]),
-                                 row_bcast<0>(w[1]), row_bcast<1>(w[1]), row_bcast<2>(w[1]), row_bcast<3>(w[1])};
-            make_operands<NB, F>(vh, st.v, EV - e_v);
 #pragma unroll
-            for (int i = 0; i < NR; ++i) {
-                half8 xh, xl;
+            for (int h = 0; h < 2; ++h) {
+                const float wc[8] = {row_bcast<0>(w[2 * h]), row_bcast<1>(w[2 * h]), row_bcast<2>(w[2 * h]), row_bcast<3>(w[2 * h]),
+                                     row_bcast<0>(w[2 * h + 1]), row_bcast<1>(w[2 * h + 1]), row_bcast<2>(w[2 * h + 1]), row_bcast<3>(w[2 * h + 1])};
+                half8 x[NR], xl[NR], w8;                  // (xl with two terms, w8 with one)
+                if constexpr (!TWO) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    const float k = (float)kh[row[i]][c];
-                    xh[c] = (_Float16)(wc[c] * k);
-                    xl[c] = (_Float16)fmaf(wc[c], k, -(float)xh[c]);
-                    mu[i] = fmaf(wc[c], k, mu[i]);
-                    yv[i] = fmaf(wc[c], (float)vh[row[i]][c], yv[i]);
+                    for (int c = 0; c < 8; ++c) w8[c] = (_Float16)wc[c];
                 }
-                auto product = [&](f32x4 &t, const half8 &b) { t = mfma_f16(xh, b, mfma_f16(xl, b, t)); };
 #pragma unroll
-                for (int J = row[i]; J < NB; ++J) product(acc[upper_tile<NB>(row[i], J)], kh[J]);
+                for (int i = 0; i < NR; ++i) {
+                    if constexpr (!TWO) {
+                        x[i] = w8 * kown[h][i];
+                        mu[i] = dot8(w8, kown[h][i], mu[i]);
+                    } else {
 #pragma unroll
-                for (int J = 0; J < NB; ++J) product(acc[S::NSIG + NB * row[i] + J], vh[J]);
+                        for (int c = 0; c < 8; ++c) {
+                            const float kf = (float)kown[h][i][c];
+                            x[i][c] = (_Float16)(wc[c] * kf);
+                            xl[i][c] = (_Float16)fmaf(wc[c], kf, -(float)x[i][c]);
+                            mu[i] = fmaf(wc[c], kf, mu[i]);
+                        }
+                    }
+                }
+                auto product = [&](int i, const half8 &b, f32x4 &sum) {
+                    if constexpr (!TWO) sum = mfma_f16(x[i], b, sum);
+                    else sum += mfma_f16(x[i], b, mfma_f16(xl[i], b, f32x4{0.f, 0.f, 0.f, 0.f}));
+                };
+#pragma unroll
+                for (int i = 0; i < NR; ++i) {
+                    pin(mu[i]);
+                    pin(x[i]);
+                    if constexpr (TWO) pin(xl[i]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int J = low; J < NB; ++J) {
+                    const half8 b = J == row[0] ? kown[h][0] : J == row[1] ? kown[h][1] : operand<F>(read(s, 0, h, J), pk);
+#pragma unroll
+                    for (int i = 0; i < NR; ++i)
+                        if (J >= row[i]) product(i, b, acc[upper_tile<NB>(row[i], J)]);
+                    if (J % 2) __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int J = 0; J < NB; ++J) {
+                    const half8 v = operand<F>(read(s, 1, h, J), pv);
+#pragma unroll
+                    for (int i = 0; i < NR; ++i) {
+                        if (J == row[i]) {
+                            if constexpr (!TWO) yv[i] = dot8(w8, v, yv[i]);
+                            else {
+#pragma unroll
+                                for (int c = 0; c < 8; ++c) yv[i] = fmaf(wc[c], (float)v[c], yv[i]);
+                            }
+                        }
+                        product(i, v, acc[S::NSIG + NB * row[i] + J]);
+                    }
+                    if (J == row[0]) pin(yv[0]);
+                    if (J == row[1]) pin(yv[1]);
+                    if (J % 2) __builtin_amdgcn_sched_barrier(0);
+                }
             }
-        };
-        for (int s = 0; s < nsteps; s += 2) {
-            load(sb, s + 1);
-            compute(sa, s);
-            load(sa, s + 2);
-            if (s + 1 < nsteps) compute(sb, s + 1);
+            if (s + 1 < nsteps) partial_logits(s + 1);
         }
         for_tiles([&](int t, bool sigma) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[t][i] = __builtin_ldexpf(acc[t][i], EK + U::EXP + (sigma ? EK : EV) + U::EXP);
+            for (int i = 0; i < 4; ++i) acc[t][i] = __builtin_ldexpf(acc[t][i], EK + U + (sigma ? EK : EV) + U);
         });
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            mu[i] = __builtin_ldexpf(mu[i], EK + U::EXP);
-            yv[i] = __builtin_ldexpf(yv[i], EV + U::EXP);
+            mu[i] = __builtin_ldexpf(mu[i], EK + U);
+            yv[i] = __builtin_ldexpf(yv[i], EV + U);
         }
     }
 
@@ -308,48 +628,59 @@ __device__ __forceinline__ void decode_q8_body(const Q8Args &a, const DecPiece &
     om = rows_allsum(om);
 #pragma unroll
     for (int i = 0; i < NR; ++i) { mu[i] = rows_allsum(mu[i]); yv[i] = rows_allsum(yv[i]); }
-    float *R = a.parts + (size_t)pc.rec * S::REC_F;       // this workgroup's record (not FUSED)
-    if constexpr (!S::TEAM) {
-        finish_workgroup<D, TQ, true, FUSED, S::NBUF>(lds, acc, mu, yv, om, mref, mtrue, R, a.out, bh, wave, lane);
-    } else {                                              // every wave's own tiles, relative to the true maximum
-        const float f = mref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mref - mtrue);
-        float *tiles, *mud, *yvd;
-        if constexpr (FUSED) { tiles = lds.tiles[0]; mud = lds.mu[0]; yvd = lds.yv[0]; }
-        else { tiles = R + S::HDR; mud = R + 64; yvd = R + 64 + D; }
-        for_tiles([&](int t, bool) { *reinterpret_cast<f32x4 *>(tiles + t * 256 + lane * 4) = f * acc[t]; });
-        if (g == 0) {
+    if constexpr (FUSED) __syncthreads();                 // the rows are dead: the moments take their place
+    // every wave's own tiles, relative to the true maximum
+    const float f = mref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mref - mtrue);
+    float *R = a.parts + (size_t)pc.rec * S::REC_F, *tiles, *mud, *yvd;
+    if constexpr (FUSED) { tiles = lds.tiles[0]; mud = lds.mu[0]; yvd = lds.yv[0]; }
+    else { tiles = R + S::HDR; mud = R + 64; yvd = R + 64 + D; }
+    for_tiles([&](int t, bool) { *reinterpret_cast<f32x4 *>(tiles + t * 256 + lane * 4) = f * acc[t]; });
+    if (g == 0) {
 #pragma unroll
-            for (int i = 0; i < NR; ++i) { mud[16 * row[i] + nn] = f * mu[i]; yvd[16 * row[i] + nn] = f * yv[i]; }
-        }
-        if (W == 0 && lane == 0) {
-            if constexpr (FUSED) lds.om[0] = f * om;
-            else { R[0] = mtrue; R[1] = f * om; }
-        }
-        if constexpr (FUSED) {
-            const QueryPart<D> query = load_query<D, TQ, true>(a.out, bh, lane);
-            __syncthreads();
-            solve_head<D, TQ, true>(lds, a.out, query, bh, wave, lane);
-        }
+        for (int i = 0; i < NR; ++i) { mud[16 * row[i] + nn] = f * mu[i]; yvd[16 * row[i] + nn] = f * yv[i]; }
+    }
+    if (W == 0 && lane == 0) {
+        if constexpr (FUSED) lds.om[0] = f * om;
+        else { R[0] = mtrue; R[1] = f * om; }
+    }
+    if constexpr (FUSED) {
+        const QueryPart<D> query = load_query<D, TQ, false>(a.out, bh, lane);
+        __syncthreads();
+        solve_head<D, TQ, false>(lds, a.out, query, bh, wave, lane);
     }
 }
 
 template <int D, typename F, typename TQ, bool FUSED>
-__global__ __launch_bounds__(NT, D <= 32 ? 4 : (D == 128 && FUSED) ? 1 : 2) void decode_q8_kernel(Q8Args a)
+__global__ __launch_bounds__(NT, (D == 128 && FUSED) ? 1 : 2) void decode_q8_kernel(Q8Args a)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     using S = Q8Shape<D>;
     if constexpr (S::TEAM) {                              // scalar branches; all four waves meet at the same barriers
-        __shared__ __align__(16) unsigned char raw[FUSED ? sizeof(HeadLds<D, 1, 1>) : 16];
-        HeadLds<D, 1, 1> &lds = *reinterpret_cast<HeadLds<D, 1, 1> *>(raw);
+        using Lds = HeadLds<D, 1, 1>;
+        constexpr size_t BYTES = FUSED && sizeof(Lds) > sizeof(WideLds) ? sizeof(Lds) : sizeof(WideLds);
+        __shared__ __align__(16) unsigned char raw[BYTES];
+        Lds &lds = *reinterpret_cast<Lds *>(raw);
+        WideLds &wl = *reinterpret_cast<WideLds *>(raw);
         for_pieces<FUSED>(a.split, [&](const DecPiece &pc) {
-            if (wave == 0) decode_q8_body<D, F, TQ, FUSED, 0>(a, pc, lds, wave, piece_lane());
-            else if (wave == 1) decode_q8_body<D, F, TQ, FUSED, 1>(a, pc, lds, wave, piece_lane());
-            else if (wave == 2) decode_q8_body<D, F, TQ, FUSED, 2>(a, pc, lds, wave, piece_lane());
-            else decode_q8_body<D, F, TQ, FUSED, 3>(a, pc, lds, wave, piece_lane());
+            auto with = [&](auto two) {
+                constexpr bool TWO = decltype(two)::value;
+                if (wave == 0) decode_q8_wide_body<F, TQ, FUSED, TWO, 0>(a, pc, lds, wl, wave, piece_lane());
+                else if (wave == 1) decode_q8_wide_body<F, TQ, FUSED, TWO, 1>(a, pc, lds, wl, wave, piece_lane());
+                else if (wave == 2) decode_q8_wide_body<F, TQ, FUSED, TWO, 2>(a, pc, lds, wl, wave, piece_lane());
+                else decode_q8_wide_body<F, TQ, FUSED, TWO, 3>(a, pc, lds, wl, wave, piece_lane());
+            };
+            if (!a.out.out_bf16 || pc.L <= 4 * D) with(std::true_type{});
+            else with(std::false_type{});
         });
     } else {
-        __shared__ HeadLds<D, S::NBUF, 4> lds;
-        for_pieces<FUSED>(a.split, [&](const DecPiece &pc) { decode_q8_body<D, F, TQ, FUSED, 0>(a, pc, lds, wave, piece_lane()); });
+        using Lds = HeadLds<D, S::NBUF, 4>;
+        constexpr size_t STAGES_B = (size_t)4 * S::STAGES * 2 * S::TILE_B;
+        __shared__ __align__(16) unsigned char raw[STAGES_B > sizeof(Lds) ? STAGES_B : sizeof(Lds)];
+        Lds &lds = *reinterpret_cast<Lds *>(raw);
+        for_pieces<FUSED>(a.split, [&](const DecPiece &pc) {
+            if (!a.out.out_bf16 || pc.L <= 4 * D) decode_q8_body<D, F, TQ, FUSED, true>(a, pc, lds, raw, wave, piece_lane());
+            else decode_q8_body<D, F, TQ, FUSED, false>(a, pc, lds, raw, wave, piece_lane());
+        });
     }
 }
 
@@ -394,7 +725,7 @@ __global__ __launch_bounds__(NT, D == 128 ? 1 : 2) void merge_q8_kernel(Q8Args a
         return;
     }
     if (seq_len(a.split, blockIdx.x / a.split.H) <= DUAL_MAX_KEYS) return;
-    merge_head<D, TQ, true>(*reinterpret_cast<HeadLds<D, 1, 1> *>(raw), a.split, a.out, a.parts, blockIdx.x);
+    merge_head<D, TQ, false>(*reinterpret_cast<HeadLds<D, 1, 1> *>(raw), a.split, a.out, a.parts, blockIdx.x);
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------------------------
