@@ -48,7 +48,7 @@ struct Q8Shape : DecShape<D> {
     static constexpr int NR = TEAM ? 2 : D / 16;          // row blocks of a wave
     static constexpr int NBUF = D <= 32 ? 4 : TEAM ? 1 : 2;
     static constexpr int KEYS_MIN = TEAM ? 256 : 512;     // fewest keys worth a workgroup
-    static constexpr int SLOTS = 512;                     // workgroups worth having at once
+    static constexpr int SLOTS = D <= 32 ? 1024 : 512;    // workgroups worth having at once
     static constexpr int MAX_SPLIT = 32;
     static constexpr int CPR = D / 16;                    // 16-byte chunks of a row
     static constexpr int TILE_B = KEYS * D;               // keys or values of a stage
@@ -119,6 +119,14 @@ __device__ __forceinline__ float reduce4(const float *p, int nn)
     return s;
 }
 
+// pairs of lanes 0 to 3 of the row
+__device__ __forceinline__ half8 pair_bcast(half2q p)
+{
+    const float f = __builtin_bit_cast(float, p);
+    const f32x4 v = {row_bcast<0>(f), row_bcast<1>(f), row_bcast<2>(f), row_bcast<3>(f)};
+    return __builtin_bit_cast(half8, v);
+}
+
 // sum of a[0..7] b[0..7] onto c (v_dot2_f32_f16: exact products)
 __device__ __forceinline__ float dot8(half8 a, half8 b, float c)
 {
@@ -134,6 +142,17 @@ __device__ __forceinline__ float dot8(half8 a, half8 b, float c)
 __device__ __forceinline__ void pin(half8 &x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void pin(f32x4 &x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void pin(float &x) { asm volatile("" : "+v"(x)); }
+
+// w k = h + l in two f16.  h is pinned between the two: the compiler (ROCm 7.2) otherwise forms some of its elements twice, for the operand from the
+// product rounded to fp32 and for the remainder from the exact one (v_fma_mixlo), and where the two roundings differ, once in 2^14, h + l is off by 2^-11.
+__device__ __forceinline__ void two_terms(const float (&w)[8], const half8 &k, half8 &h, half8 &l)
+{
+#pragma unroll
+    for (int c = 0; c < 8; ++c) h[c] = (_Float16)(w[c] * (float)k[c]);
+    pin(h);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) l[c] = (_Float16)fmaf(w[c], (float)k[c], -(float)h[c]);
+}
 
 struct Q8Args {
     const char *K, *V;
@@ -167,8 +186,11 @@ __device__ __forceinline__ void decode_q8_body(const Q8Args &a, const DecPiece &
     const int64_t krow = a.sk.seq, vrow = a.sv.seq;
     const int8_t *ke = a.ke + (size_t)(b * a.HC + hc) * a.blocks + b0, *ve = a.ve + (size_t)(b * a.HC + hc) * a.blocks + b0;
 
-    f32x4 acc[S::NTILES];
+    // one term: mu~ and sum w v come from the matrix cores too, as products with a row block of weights (in every row of muw, yvw)
+    f32x4 acc[S::NTILES], muw[NB], yvw[NB];
     float mu[NB], yv[NB], q[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) muw[i] = yvw[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < S::NTILES; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -187,24 +209,23 @@ __device__ __forceinline__ void decode_q8_body(const Q8Args &a, const DecPiece &
     // of its share and wraps around.
     const int rot = nsteps > 0 ? __builtin_amdgcn_readfirstlane((int)(((unsigned)pc.rec * 4u + wave) * 7u % (unsigned)nsteps)) : 0;
     auto block_of = [&](int s) { const int t = s + rot; return t >= nsteps ? t - nsteps : t; };
-    auto fetch = [&](int s, int stage) {
+    auto fetch = [&](int s, int stage, int tile) {        // tile: 0 keys, 1 values
         const int j0 = r0 + block_of(s) * KEYS;
-        const unsigned dst = mine_off + (unsigned)(stage * 2 * S::TILE_B);
+        const unsigned dst = mine_off + (unsigned)((2 * stage + tile) * S::TILE_B);
+        const char *X = tile ? Vh : Kh;
+        const int64_t pitch = tile ? vrow : krow;
         if (j0 + KEYS <= L) {
-            const char *kp = Kh + j0 * krow, *vp = Vh + j0 * vrow;
+            const char *p = X + j0 * pitch;
 #pragma unroll
-            for (int t = 0; t < DMAS; ++t) dma16_base_nt_off(kp + t * KPD * krow, koff, dst + 1024u * t);
-#pragma unroll
-            for (int t = 0; t < DMAS; ++t) dma16_base_nt_off(vp + t * KPD * vrow, voff, dst + S::TILE_B + 1024u * t);
+            for (int t = 0; t < DMAS; ++t) dma16_base_nt_off(p + t * KPD * pitch, tile ? voff : koff, dst + 1024u * t);
         } else {                                          // rows beyond the sequence: its last row (their weights are 0)
 #pragma unroll
-            for (int t = 0; t < DMAS; ++t) dma16_nt_off(Kh + min(j0 + t * KPD + dkey, L - 1) * krow + 16 * dchunk, dst + 1024u * t);
-#pragma unroll
-            for (int t = 0; t < DMAS; ++t) dma16_nt_off(Vh + min(j0 + t * KPD + dkey, L - 1) * vrow + 16 * dchunk, dst + S::TILE_B + 1024u * t);
+            for (int t = 0; t < DMAS; ++t) dma16_nt_off(X + min(j0 + t * KPD + dkey, L - 1) * pitch + 16 * dchunk, dst + 1024u * t);
         }
     };
-    // transposed reads: lane (g, j) addresses eight bytes of key 8 g + j / 2 and receives eight keys of feature 16 I + j
-    const int tkey = 8 * g + nn / 2, turn = D == 64 ? (tkey >> 2) & 3 : D == 32 ? (tkey >> 3) & 1 : 0;
+    // transposed reads: lane (g, j) addresses eight bytes of one key and receives eight keys of feature 16 I + j: slot 2 e + c is key 8 g + 4 c + e, so
+    // that a pair of slots is a pair of weights of one lane (below)
+    const int tkey = 8 * g + 4 * ((nn / 2) & 1) + nn / 4, turn = D == 64 ? (tkey >> 2) & 3 : D == 32 ? (tkey >> 3) & 1 : 0;
     auto read = [&](int stage, int tile, int half, int I) {
         const unsigned at = (unsigned)(tkey * D + 16 * (I ^ turn) + 8 * (nn & 1));
         const unsigned char *p = mine + stage * 2 * S::TILE_B + tile * S::TILE_B + half * 32 * D;
@@ -212,8 +233,10 @@ __device__ __forceinline__ void decode_q8_body(const Q8Args &a, const DecPiece &
     };
 
     if (nsteps > 0) {
-        fetch(0, 0);
-        if (nsteps > 1) fetch(1, 1);
+        // in the order in which they are waited for
+        fetch(0, 0, 0);
+        fetch(0, 0, 1);
+        if (nsteps > 1) { fetch(1, 1, 0); fetch(1, 1, 1); }
         {
             const TQ *qp = static_cast<const TQ *>(a.out.q) + (size_t)bh * D + nn;
 #pragma unroll
@@ -248,13 +271,17 @@ __device__ __forceinline__ void decode_q8_body(const Q8Args &a, const DecPiece &
             }
             const int e_k = __builtin_amdgcn_readlane(ek64, blk % 64), e_v = __builtin_amdgcn_readlane(ev64, blk % 64);
             const BlockPower pk = block_power<F>(EK - e_k), pv = block_power<F>(EV - e_v);
-            if (s + 1 < nsteps) wait_but<2 * DMAS>();
-            else wait_but<0>();
+            if (s + 1 < nsteps) wait_but<3 * DMAS>();     // all but this block's values and the next block
+            else wait_but<DMAS>();
             half8 k[2][NB];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int I = 0; I < NB; ++I) k[h][I] = operand<F>(read(stage, 0, h, I), pk);
+            if (s + 2 < nsteps) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // read before the transfer that overwrites them is requested
+                fetch(s + 2, stage, 0);
+            }
             float t[4];                                   // logit (log2 units) of key 32 h + 8 g + 4 c + (n % 4) in t[2 h + c]
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -265,7 +292,7 @@ __device__ __forceinline__ void decode_q8_body(const Q8Args &a, const DecPiece &
                     for (int e = 0; e < 4; ++e) {
                         p[e] = 0.f;
 #pragma unroll
-                        for (int I = 0; I < NB; ++I) p[e] = fmaf((float)k[h][I][4 * c + e], q[I], p[e]);
+                        for (int I = 0; I < NB; ++I) p[e] = fmaf((float)k[h][I][2 * e + c], q[I], p[e]);
                     }
                     t[2 * h + c] = reduce4(p, nn);
                 }
@@ -274,8 +301,10 @@ __device__ __forceinline__ void decode_q8_body(const Q8Args &a, const DecPiece &
 #pragma unroll
                 for (int I = 0; I < NB; ++I) pin(k[h][I]);
             if (e_k == EXP_NAN || e_v == EXP_NAN) t[0] = t[1] = t[2] = t[3] = NAN;      // (a scalar branch)
+            if (j0 + KEYS > r1) {                         // (scalar branches)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) t[i] = j0 + 32 * (i / 2) + 8 * g + 4 * (i % 2) + (nn & 3) < r1 ? t[i] : -INFINITY;
+                for (int i = 0; i < 4; ++i) t[i] = j0 + 32 * (i / 2) + 8 * g + 4 * (i % 2) + (nn & 3) < r1 ? t[i] : -INFINITY;
+            }
             const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
             if (__builtin_amdgcn_ballot_w64(top > mref + (TOP<TWO> + SLACK)) != 0) {
                 const float mnew = wave_max_dpp(top) - TOP<TWO>;
@@ -283,7 +312,10 @@ __device__ __forceinline__ void decode_q8_body(const Q8Args &a, const DecPiece &
                 mref = mnew;
                 om *= alpha;
 #pragma unroll
-                for (int i = 0; i < NB; ++i) { mu[i] *= alpha; yv[i] *= alpha; }
+                for (int i = 0; i < NB; ++i) {
+                    if constexpr (TWO) { mu[i] *= alpha; yv[i] *= alpha; }
+                    else { muw[i] *= alpha; yvw[i] *= alpha; }
+                }
 #pragma unroll
                 for (int i = 0; i < S::NTILES; ++i) acc[i] *= alpha;
             }
@@ -295,66 +327,78 @@ __device__ __forceinline__ void decode_q8_body(const Q8Args &a, const DecPiece &
                 if constexpr (!TWO) w[i] = (float)(_Float16)w[i];
                 om += w[i];
             }
-            auto spread = [&](int h, float (&o)[8]) {                 // the weights of a half's keys in the operands' order
-                o[0] = row_bcast<0>(w[2 * h]); o[1] = row_bcast<1>(w[2 * h]); o[2] = row_bcast<2>(w[2 * h]); o[3] = row_bcast<3>(w[2 * h]);
-                o[4] = row_bcast<0>(w[2 * h + 1]); o[5] = row_bcast<1>(w[2 * h + 1]); o[6] = row_bcast<2>(w[2 * h + 1]); o[7] = row_bcast<3>(w[2 * h + 1]);
-            };
+            if (s + 2 < nsteps) wait_but<3 * DMAS>();     // all but the next block and the keys of the one after it
+            else if (s + 1 < nsteps) wait_but<2 * DMAS>();
+            else wait_but<0>();
             // (the scheduler is kept inside one block of features: left to itself it reads and converts the whole stage first and spills)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                float wc[8];
-                spread(h, wc);
-                half8 w8, x[NB], xl[NB];                  // (w8 with one term, xl with two)
-                if constexpr (!TWO) {
+                int2q raw[NB];                            // values, on their way while the keys are multiplied
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) w8[c] = (_Float16)wc[c];
+                for (int J = 0; J < NB; ++J) raw[J] = read(stage, 1, h, J);
+                half8 w8, x[NB], xl[NB];                  // the half's weights in the operands' order: w8 with one term, wc (and xl) with two
+                float wc[8];
+                if constexpr (!TWO) w8 = pair_bcast(half2q{(_Float16)w[2 * h], (_Float16)w[2 * h + 1]});
+                else {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        wc[c] = row_bcast<0>(w[2 * h + c]);
+                        wc[2 + c] = row_bcast<1>(w[2 * h + c]);
+                        wc[4 + c] = row_bcast<2>(w[2 * h + c]);
+                        wc[6 + c] = row_bcast<3>(w[2 * h + c]);
+                    }
                 }
                 auto product = [&](int I, const half8 &b, f32x4 &sum) {
                     if constexpr (!TWO) sum = mfma_f16(x[I], b, sum);
-                    else sum += mfma_f16(x[I], b, mfma_f16(xl[I], b, f32x4{0.f, 0.f, 0.f, 0.f}));
+                    else {
+                        sum += mfma_f16(x[I], b, mfma_f16(xl[I], b, f32x4{0.f, 0.f, 0.f, 0.f}));
+                        pin(sum);
+                    }
                 };
 #pragma unroll
                 for (int J = 0; J < NB; ++J) {
                     if constexpr (!TWO) {
                         x[J] = w8 * k[h][J];
-                        mu[J] = dot8(w8, k[h][J], mu[J]);
+                        muw[J] = mfma_f16(w8, k[h][J], muw[J]);
                     } else {
+                        two_terms(wc, k[h][J], x[J], xl[J]);
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            const float kf = (float)k[h][J][c];
-                            x[J][c] = (_Float16)(wc[c] * kf);
-                            xl[J][c] = (_Float16)fmaf(wc[c], kf, -(float)x[J][c]);
-                            mu[J] = fmaf(wc[c], kf, mu[J]);
-                        }
+                        for (int c = 0; c < 8; ++c) mu[J] = fmaf(wc[c], (float)k[h][J][c], mu[J]);
                     }
 #pragma unroll
                     for (int I = 0; I <= J; ++I) product(I, k[h][J], acc[upper_tile<NB>(I, J)]);
-                    pin(mu[J]);
+                    if constexpr (TWO) pin(mu[J]);
                     pin(x[J]);
                     if constexpr (TWO) pin(xl[J]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
 #pragma unroll
                 for (int J = 0; J < NB; ++J) {
-                    const half8 v = operand<F>(read(stage, 1, h, J), pv);
-                    if constexpr (!TWO) yv[J] = dot8(w8, v, yv[J]);
+                    const half8 v = operand<F>(raw[J], pv);
+                    if constexpr (!TWO) yvw[J] = mfma_f16(w8, v, yvw[J]);
                     else {
 #pragma unroll
                         for (int c = 0; c < 8; ++c) yv[J] = fmaf(wc[c], (float)v[c], yv[J]);
                     }
 #pragma unroll
                     for (int I = 0; I < NB; ++I) product(I, v, acc[S::NSIG + NB * I + J]);
-                    pin(yv[J]);
+                    if constexpr (TWO) pin(yv[J]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // read before the transfer that overwrites them is requested
-            if (s + 2 < nsteps) fetch(s + 2, stage);
+            if (s + 2 < nsteps) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                fetch(s + 2, stage, 1);
+            }
         };
 #pragma unroll 1
         for (int s = 0; s < nsteps; s += 2) {
             compute(s, std::integral_constant<int, 0>{});
             if (s + 1 < nsteps) compute(s + 1, std::integral_constant<int, 1>{});
+        }
+        if constexpr (!TWO) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) { mu[i] = 0.25f * muw[i][0]; yv[i] = 0.25f * yvw[i][0]; }      // (summed over the four groups below)
         }
         // back from the operands' scale
 #pragma unroll
@@ -562,18 +606,17 @@ __device__ __forceinline__ void decode_q8_wide_body(const Q8Args &a, const DecPi
                         x[i] = w8 * kown[h][i];
                         mu[i] = dot8(w8, kown[h][i], mu[i]);
                     } else {
+                        two_terms(wc, kown[h][i], x[i], xl[i]);
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            const float kf = (float)kown[h][i][c];
-                            x[i][c] = (_Float16)(wc[c] * kf);
-                            xl[i][c] = (_Float16)fmaf(wc[c], kf, -(float)x[i][c]);
-                            mu[i] = fmaf(wc[c], kf, mu[i]);
-                        }
+                        for (int c = 0; c < 8; ++c) mu[i] = fmaf(wc[c], (float)kown[h][i][c], mu[i]);
                     }
                 }
                 auto product = [&](int i, const half8 &b, f32x4 &sum) {
                     if constexpr (!TWO) sum = mfma_f16(x[i], b, sum);
-                    else sum += mfma_f16(x[i], b, mfma_f16(xl[i], b, f32x4{0.f, 0.f, 0.f, 0.f}));
+                    else {
+                        sum += mfma_f16(x[i], b, mfma_f16(xl[i], b, f32x4{0.f, 0.f, 0.f, 0.f}));
+                        pin(sum);
+                    }
                 };
 #pragma unroll
                 for (int i = 0; i < NR; ++i) {
@@ -650,38 +693,41 @@ __device__ __forceinline__ void decode_q8_wide_body(const Q8Args &a, const DecPi
     }
 }
 
-template <int D, typename F, typename TQ, bool FUSED>
+// LDS of a workgroup: the stages of its waves, later the moments
+template <int D, bool FUSED>
+struct Q8Lds {
+    using S = Q8Shape<D>;
+    using Head = HeadLds<D, S::NBUF, S::TEAM ? 1 : 4>;
+    static constexpr size_t STAGES_B = S::TEAM ? sizeof(WideLds) : (size_t)4 * S::STAGES * 2 * S::TILE_B;
+    static constexpr size_t BYTES = (FUSED || !S::TEAM) && sizeof(Head) > STAGES_B ? sizeof(Head) : STAGES_B;
+};
+
+template <int D, typename F, typename TQ, bool FUSED, bool TWO>
+__device__ __forceinline__ void decode_q8_piece(const Q8Args &a, const DecPiece &pc, unsigned char *raw, int wave)
+{
+    auto &lds = *reinterpret_cast<typename Q8Lds<D, FUSED>::Head *>(raw);
+    if constexpr (D == 128) {                             // scalar branches; all four waves meet at the same barriers
+        WideLds &wl = *reinterpret_cast<WideLds *>(raw);
+        if (wave == 0) decode_q8_wide_body<F, TQ, FUSED, TWO, 0>(a, pc, lds, wl, wave, piece_lane());
+        else if (wave == 1) decode_q8_wide_body<F, TQ, FUSED, TWO, 1>(a, pc, lds, wl, wave, piece_lane());
+        else if (wave == 2) decode_q8_wide_body<F, TQ, FUSED, TWO, 2>(a, pc, lds, wl, wave, piece_lane());
+        else decode_q8_wide_body<F, TQ, FUSED, TWO, 3>(a, pc, lds, wl, wave, piece_lane());
+    } else {
+        decode_q8_body<D, F, TQ, FUSED, TWO>(a, pc, lds, raw, wave, piece_lane());
+    }
+}
+
+// One term: sequences of at most PRECISE_KEYS are left to precise_heads_kernel.  (Both variants in one kernel spilled, and with spills around its
+// transfers one of them gave wrong moments.)
+template <int D> constexpr int PRECISE_KEYS = 4 * D;
+template <int D, typename F, typename TQ, bool FUSED, bool TWO>
 __global__ __launch_bounds__(NT, (D == 128 && FUSED) ? 1 : 2) void decode_q8_kernel(Q8Args a)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    using S = Q8Shape<D>;
-    if constexpr (S::TEAM) {                              // scalar branches; all four waves meet at the same barriers
-        using Lds = HeadLds<D, 1, 1>;
-        constexpr size_t BYTES = FUSED && sizeof(Lds) > sizeof(WideLds) ? sizeof(Lds) : sizeof(WideLds);
-        __shared__ __align__(16) unsigned char raw[BYTES];
-        Lds &lds = *reinterpret_cast<Lds *>(raw);
-        WideLds &wl = *reinterpret_cast<WideLds *>(raw);
-        for_pieces<FUSED>(a.split, [&](const DecPiece &pc) {
-            auto with = [&](auto two) {
-                constexpr bool TWO = decltype(two)::value;
-                if (wave == 0) decode_q8_wide_body<F, TQ, FUSED, TWO, 0>(a, pc, lds, wl, wave, piece_lane());
-                else if (wave == 1) decode_q8_wide_body<F, TQ, FUSED, TWO, 1>(a, pc, lds, wl, wave, piece_lane());
-                else if (wave == 2) decode_q8_wide_body<F, TQ, FUSED, TWO, 2>(a, pc, lds, wl, wave, piece_lane());
-                else decode_q8_wide_body<F, TQ, FUSED, TWO, 3>(a, pc, lds, wl, wave, piece_lane());
-            };
-            if (!a.out.out_bf16 || pc.L <= 4 * D) with(std::true_type{});
-            else with(std::false_type{});
-        });
-    } else {
-        using Lds = HeadLds<D, S::NBUF, 4>;
-        constexpr size_t STAGES_B = (size_t)4 * S::STAGES * 2 * S::TILE_B;
-        __shared__ __align__(16) unsigned char raw[STAGES_B > sizeof(Lds) ? STAGES_B : sizeof(Lds)];
-        Lds &lds = *reinterpret_cast<Lds *>(raw);
-        for_pieces<FUSED>(a.split, [&](const DecPiece &pc) {
-            if (!a.out.out_bf16 || pc.L <= 4 * D) decode_q8_body<D, F, TQ, FUSED, true>(a, pc, lds, raw, wave, piece_lane());
-            else decode_q8_body<D, F, TQ, FUSED, false>(a, pc, lds, raw, wave, piece_lane());
-        });
-    }
+    __shared__ __align__(16) unsigned char raw[Q8Lds<D, FUSED>::BYTES];
+    for_pieces<FUSED>(a.split, [&](const DecPiece &pc) {
+        if (TWO || pc.L > PRECISE_KEYS<D>) decode_q8_piece<D, F, TQ, FUSED, TWO>(a, pc, raw, wave);
+    });
 }
 
 // Sequences of at most 64 keys, which one block of the format holds: in key space (llla_dual.hpp); empty ones give zeros
@@ -703,29 +749,29 @@ __device__ __forceinline__ void short_head(dual::DualShared<D, DUAL_MAX_KEYS> &s
                               nullptr, nullptr);
 }
 
+// Sequences that the kernels proper leave: one workgroup per head.  precise: also those that one term is too little for.
 template <int D, typename F, typename TQ>
-__global__ __launch_bounds__(NT) void short_heads_kernel(Q8Args a, float scale)
-{
-    __shared__ dual::DualShared<D, DUAL_MAX_KEYS> sm;
-    if (a.out.out_bf16) short_head<D, F, TQ, bf16_t>(sm, a, scale, blockIdx.x);
-    else short_head<D, F, TQ, float>(sm, a, scale, blockIdx.x);
-}
-
-// Merge of the records, one workgroup per head, and behind them one per head for short sequences; which of the two writes the head follows from
-// its length
-template <int D, typename F, typename TQ>
-__global__ __launch_bounds__(NT, D == 128 ? 1 : 2) void merge_q8_kernel(Q8Args a, float scale, int heads)
+__global__ __launch_bounds__(NT) void precise_heads_kernel(Q8Args a, float scale, int precise)
 {
     using Dual = dual::DualShared<D, DUAL_MAX_KEYS>;
-    constexpr size_t LDS_B = sizeof(HeadLds<D, 1, 1>) > sizeof(Dual) ? sizeof(HeadLds<D, 1, 1>) : sizeof(Dual);
-    __shared__ __align__(16) unsigned char raw[LDS_B];
-    if ((int)blockIdx.x >= heads) {
-        if (a.out.out_bf16) short_head<D, F, TQ, bf16_t>(*reinterpret_cast<Dual *>(raw), a, scale, blockIdx.x - heads);
-        else short_head<D, F, TQ, float>(*reinterpret_cast<Dual *>(raw), a, scale, blockIdx.x - heads);
-        return;
+    __shared__ __align__(16) unsigned char raw[Q8Lds<D, true>::BYTES > sizeof(Dual) ? Q8Lds<D, true>::BYTES : sizeof(Dual)];
+    const int bh = blockIdx.x, H = a.split.H, L = __builtin_amdgcn_readfirstlane(cache_length(a.split.seqlens, bh / H, a.split.L_max));
+    if (L <= DUAL_MAX_KEYS) {
+        if (a.out.out_bf16) short_head<D, F, TQ, bf16_t>(*reinterpret_cast<Dual *>(raw), a, scale, bh);
+        else short_head<D, F, TQ, float>(*reinterpret_cast<Dual *>(raw), a, scale, bh);
+    } else if (precise && L <= PRECISE_KEYS<D>) {
+        const DecPiece pc{bh / H, bh % H, bh, L, 0, L, bh};
+        decode_q8_piece<D, F, TQ, true, true>(a, pc, raw, __builtin_amdgcn_readfirstlane(threadIdx.x / 64));
     }
-    if (seq_len(a.split, blockIdx.x / a.split.H) <= DUAL_MAX_KEYS) return;
-    merge_head<D, TQ, false>(*reinterpret_cast<HeadLds<D, 1, 1> *>(raw), a.split, a.out, a.parts, blockIdx.x);
+}
+
+// Merge of the records, one workgroup per head; least: shorter sequences are not of this call's
+template <int D, typename TQ>
+__global__ __launch_bounds__(NT, D == 128 ? 1 : 2) void merge_q8_kernel(DecSplit split, HeadOut out, const float *__restrict__ parts, int least)
+{
+    __shared__ HeadLds<D, 1, 1> lds;
+    if (seq_len(split, blockIdx.x / split.H) <= least) return;
+    merge_head<D, TQ, false>(lds, split, out, parts, blockIdx.x);
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------------------------
@@ -777,26 +823,33 @@ hipError_t q8_launch(const DecodeQ8Problem &p)
     a.parts = static_cast<float *>(p.ws);
     Problem cut{};
     cut.seqlens = p.seqlens; cut.B = c.B; cut.H = p.H; cut.n = c.L_max;
+    // which sequences are whose: at most DUAL_MAX_KEYS in key space; a bf16 result's others at most PRECISE_KEYS with two terms
+    const bool two = p.out != LLLA_BF16 || c.L_max <= PRECISE_KEYS<D>;
+    const int least = two ? DUAL_MAX_KEYS : PRECISE_KEYS<D>;
     if (c.L_max <= DUAL_MAX_KEYS) {
         a.split = DecSplit{p.seqlens, c.B, p.H, c.L_max, 1, 0, 0, 0, 0};
         stage_mark(p.stream, "decode_q8_short");
-        hipLaunchKernelGGL((short_heads_kernel<D, F, TQ>), dim3(bh), dim3(NT), 0, p.stream, a, p.scale);
+        hipLaunchKernelGGL((precise_heads_kernel<D, F, TQ>), dim3(bh), dim3(NT), 0, p.stream, a, p.scale, 0);
         return hipGetLastError();
     }
     const size_t records = q8_records<D>(c.B, p.H, c.L_max);
     const bool scratch = p.ws != nullptr && (reinterpret_cast<uintptr_t>(p.ws) & 255u) == 0 && p.ws_bytes >= records * S::REC_F * sizeof(float);
     const int ns = scratch ? q8_nsplit<D>(bh, c.L_max) : 1;
     a.split = choose_split(cut, ns, scratch ? records : 0, S::SLOTS, 2 * CACHE_BLOCK, S::KEYS_MIN, S::MAX_SPLIT);
-    if (a.split.nsplit == 1 && a.split.slots == 0) {
-        stage_mark(p.stream, "decode_q8");
-        hipLaunchKernelGGL((decode_q8_kernel<D, F, TQ, true>), dim3(1, bh), dim3(NT), 0, p.stream, a);
-        if (p.seqlens != nullptr) hipLaunchKernelGGL((short_heads_kernel<D, F, TQ>), dim3(bh), dim3(NT), 0, p.stream, a, p.scale);
-    } else {
-        stage_mark(p.stream, "decode_q8_partial");
-        hipLaunchKernelGGL((decode_q8_kernel<D, F, TQ, false>), a.split.slots ? dim3(a.split.slots, p.H) : dim3(a.split.nsplit, bh), dim3(NT), 0, p.stream, a);
+    const bool fused = a.split.nsplit == 1 && a.split.slots == 0;
+    const dim3 grid = fused ? dim3(1, bh) : a.split.slots ? dim3(a.split.slots, p.H) : dim3(a.split.nsplit, bh);
+    stage_mark(p.stream, fused ? "decode_q8" : "decode_q8_partial");
+    if (fused && two) hipLaunchKernelGGL((decode_q8_kernel<D, F, TQ, true, true>), grid, dim3(NT), 0, p.stream, a);
+    else if (fused) hipLaunchKernelGGL((decode_q8_kernel<D, F, TQ, true, false>), grid, dim3(NT), 0, p.stream, a);
+    else if (two) hipLaunchKernelGGL((decode_q8_kernel<D, F, TQ, false, true>), grid, dim3(NT), 0, p.stream, a);
+    else hipLaunchKernelGGL((decode_q8_kernel<D, F, TQ, false, false>), grid, dim3(NT), 0, p.stream, a);
+    if (!fused) {
         stage_mark(p.stream, "decode_q8_merge");
-        hipLaunchKernelGGL((merge_q8_kernel<D, F, TQ>), dim3(p.seqlens ? 2 * bh : bh), dim3(NT), 0, p.stream, a, p.scale, bh);
+        hipLaunchKernelGGL((merge_q8_kernel<D, TQ>), dim3(bh), dim3(NT), 0, p.stream, a.split, a.out, (const float *)a.parts, p.seqlens ? least : 0);
     }
+    // (behind the others: a fused kernel with two terms has written something for short sequences too)
+    if (p.seqlens != nullptr)
+        hipLaunchKernelGGL((precise_heads_kernel<D, F, TQ>), dim3(bh), dim3(NT), 0, p.stream, a, p.scale, two ? 0 : 1);
     return hipGetLastError();
 }
 
