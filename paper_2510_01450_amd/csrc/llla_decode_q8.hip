@@ -565,6 +565,16 @@ __device__ __forceinline__ void decode_q8_wide_body(const Q8Args &a, const DecPi
             meet(s + 2 < nsteps);
             if (s + 3 < nsteps) fetch(s + 3);
             const int j0 = r0 + block_of(s) * KEYS;
+            // a half's codes, requested long before they are multiplied: the first half's here, the second's when the first's keys are done
+            int2q kraw[NB], vraw[NB];
+            auto request = [&](int h) {
+#pragma unroll
+                for (int J = low; J < NB; ++J)
+                    if (J != row[0] && J != row[1]) kraw[J] = read(s, 0, h, J);
+#pragma unroll
+                for (int J = 0; J < NB; ++J) vraw[J] = read(s, 1, h, J);
+            };
+            request(0);
             float t[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -627,7 +637,7 @@ __device__ __forceinline__ void decode_q8_wide_body(const Q8Args &a, const DecPi
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int J = low; J < NB; ++J) {
-                    const half8 b = J == row[0] ? kown[h][0] : J == row[1] ? kown[h][1] : operand<F>(read(s, 0, h, J), pk);
+                    const half8 b = J == row[0] ? kown[h][0] : J == row[1] ? kown[h][1] : operand<F>(kraw[J], pk);
 #pragma unroll
                     for (int i = 0; i < NR; ++i)
                         if (J >= row[i]) product(i, b, acc[upper_tile<NB>(row[i], J)]);
@@ -635,7 +645,7 @@ __device__ __forceinline__ void decode_q8_wide_body(const Q8Args &a, const DecPi
                 }
 #pragma unroll
                 for (int J = 0; J < NB; ++J) {
-                    const half8 v = operand<F>(read(s, 1, h, J), pv);
+                    const half8 v = operand<F>(vraw[J], pv);
 #pragma unroll
                     for (int i = 0; i < NR; ++i) {
                         if (J == row[i]) {
@@ -651,6 +661,7 @@ __device__ __forceinline__ void decode_q8_wide_body(const Q8Args &a, const DecPi
                     if (J == row[1]) pin(yv[1]);
                     if (J % 2) __builtin_amdgcn_sched_barrier(0);
                 }
+                if (h == 0) request(1);
             }
             if (s + 1 < nsteps) partial_logits(s + 1);
         }
