@@ -33,24 +33,39 @@ struct Operand {
     bf16x8 v[CH][TERMS];
 };
 
+// a lane's part of a row as it lies in memory
 template <int D, typename T>
-__device__ __forceinline__ void load_operand(Operand<D, T> &o, const char *row, int g)
-{
-    constexpr int PER = D / 4, SIZE = RowType<T>::SIZE, BYTES = PER * SIZE, CH = Operand<D, T>::CH;
-    constexpr int N = PER < 8 ? PER : 8;                  // features of a step
+struct Words {
+    static constexpr int BYTES = D / 4 * RowType<T>::SIZE;
     unsigned w[BYTES / 4];
+};
+
+template <int D, typename T>
+__device__ __forceinline__ Words<D, T> load_words(const char *row, int g)
+{
+    constexpr int BYTES = Words<D, T>::BYTES;
+    Words<D, T> o;
     const char *p = row + g * BYTES;
-    if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const unsigned *>(p);
+    if constexpr (BYTES == 4) o.w[0] = *reinterpret_cast<const unsigned *>(p);
     else if constexpr (BYTES == 8) {
         const uint2 v = *reinterpret_cast<const uint2 *>(p);
-        w[0] = v.x; w[1] = v.y;
+        o.w[0] = v.x; o.w[1] = v.y;
     } else {
 #pragma unroll
         for (int i = 0; i < BYTES / 16; ++i) {
             const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
-            w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+            o.w[4 * i] = v.x; o.w[4 * i + 1] = v.y; o.w[4 * i + 2] = v.z; o.w[4 * i + 3] = v.w;
         }
     }
+    return o;
+}
+
+template <int D, typename T>
+__device__ __forceinline__ void make_operand(Operand<D, T> &o, const Words<D, T> &in)
+{
+    constexpr int PER = D / 4, SIZE = RowType<T>::SIZE, CH = Operand<D, T>::CH;
+    constexpr int N = PER < 8 ? PER : 8;                  // features of a step
+    const auto &w = in.w;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         if constexpr (std::is_same<T, bf16_t>::value) {
@@ -81,6 +96,19 @@ __device__ __forceinline__ void load_operand(Operand<D, T> &o, const char *row, 
     }
 }
 
+// the negative row, for a scale below zero: the largest logit is then that of the largest product too
+template <int D, typename T>
+__device__ __forceinline__ void negate(Operand<D, T> &o)
+{
+#pragma unroll
+    for (int c = 0; c < Operand<D, T>::CH; ++c)
+#pragma unroll
+        for (int i = 0; i < Operand<D, T>::TERMS; ++i) {
+            typedef unsigned u32x4q __attribute__((ext_vector_type(4)));
+            o.v[c][i] = __builtin_bit_cast(bf16x8, (u32x4q)(__builtin_bit_cast(u32x4q, o.v[c][i]) ^ 0x80008000u));
+        }
+}
+
 // 16 keys x 16 queries: lane (g, n), register t: key 4 g + t, query n
 template <int D, typename TK, typename TQ>
 __device__ __forceinline__ f32x4 logits(const Operand<D, TK> &k, const Operand<D, TQ> &q)
@@ -106,9 +134,12 @@ struct ScoresArgs {
     float *scores;
     const int32_t *seqlens;
     int HC, group, nq, M, L_max;       // M: queries of a cache head
-    int splits;                        // parts of the keys, in the statistics of few queries
-    float cscale;                      // log2(e) * scale
-    float *stats;                      // [B HC][splits][M] pairs (largest logit, sum), or with one part [B HC][M] log2 of the sums
+    int splits;                        // parts of the keys in the statistics
+    int blocks;                        // workgroups of queries there (0: a workgroup's waves share the queries)
+    float cscale;                      // log2(e) |scale|
+    int negative;                      // scale < 0
+    float *stats;                      // [B HC][splits][M] pairs (largest logit, sum)
+    float *lse;                        // [B HC][M] log2 of the sums of weights, or nullptr: merged by who needs them
     float *logits;                     // [B HC][M][pitch], or nullptr
     int64_t pitch;
 };
@@ -123,12 +154,25 @@ __device__ __forceinline__ Head head_of(const ScoresArgs &a, int bh)
     return x;
 }
 
-__device__ __forceinline__ const char *query_row(const ScoresArgs &a, const Head &x, int r)
+// Query r of a cache head: query i of query head h; beyond the last one the last (it sees nothing)
+struct Query {
+    int h, i;
+    bool real;
+    __device__ Query(const ScoresArgs &a, int r) : h(min(r, a.M - 1) / a.nq), i(min(r, a.M - 1) % a.nq), real(r < a.M) {}
+    __device__ const char *row(const ScoresArgs &a, const Head &x) const
+    {
+        return a.Q + x.b * a.sq.batch + (int64_t)(x.h * a.group + h) * a.sq.head + (int64_t)i * a.sq.seq;
+    }
+    // keys that it sees: slots below this
+    __device__ int limit(const ScoresArgs &a, const Head &x) const { return real ? x.len - a.nq + i + 1 : 0; }
+};
+
+template <int D, typename TQ>
+__device__ __forceinline__ void query_operand(Operand<D, TQ> &o, const ScoresArgs &a, const Words<D, TQ> &w)
 {
-    return a.Q + x.b * a.sq.batch + (int64_t)(x.h * a.group + r / a.nq) * a.sq.head + (int64_t)(r % a.nq) * a.sq.seq;
+    make_operand<D, TQ>(o, w);
+    if (a.negative) negate<D, TQ>(o);                     // (a scalar branch)
 }
-// keys that query r sees: slots below this
-__device__ __forceinline__ int limit_of(const ScoresArgs &a, const Head &x, int r) { return r < a.M ? x.len - a.nq + r % a.nq + 1 : 0; }
 
 // the block's power of two, times the scale of the logits
 template <typename TK>
@@ -149,72 +193,102 @@ __device__ __forceinline__ void join(float &m, float &l, float m2, float l2)
     m = top;
 }
 
+__device__ __forceinline__ int wave_min(int x)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) x = min(x, __shfl_xor(x, off));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ int wave_max(int x)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) x = max(x, __shfl_xor(x, off));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
 // Statistics of 16 RT queries per wave.  ROWS: the waves of a workgroup have queries of their own and walk through the same keys; otherwise
 // they share the queries and have parts of the keys.
+// Per logit one fused multiply-add, one exponential and one addition, and half a maximum; masks only in blocks that some query does not see whole.  Rows are
+// requested PF tiles of 16 keys ahead.
 template <int D, typename TK, typename TQ, int RT, bool ROWS>
 __global__ __launch_bounds__(NT) void stats_kernel(ScoresArgs a)
 {
+    constexpr int PF = Words<D, TK>::BYTES > 32 ? 1 : 4;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16, n = lane % 16;
     const int bh = blockIdx.y;
     const Head x = head_of(a, bh);
-    const int rb = ROWS ? (int)(gridDim.x - 1 - blockIdx.x) * NW + wave : 0, r0 = rb * 16 * RT;      // (the last queries see most: first)
+    // (the last queries see most: first)
+    const int r0 = ROWS ? ((a.blocks - 1 - (int)blockIdx.x % a.blocks) * NW + wave) * 16 * RT : 0, part = ROWS ? (int)blockIdx.x / a.blocks : (int)blockIdx.x * NW + wave;
     if (r0 >= a.M) return;
-    int k0 = 0, k1 = x.len;
-    if (!ROWS) {
-        const int part = ((x.len + a.splits - 1) / a.splits + 63) & ~63, s = blockIdx.x * NW + wave;
-        k0 = min((int64_t)s * part, (int64_t)x.len);
-        k1 = min(k0 + part, x.len);
-    }
+    const int each = ((x.len + a.splits - 1) / a.splits + 63) & ~63;
+    const int k0 = (int)min((int64_t)part * each, (int64_t)x.len);
     Operand<D, TQ> q[RT];
-    int lim[RT];
+    int lim[RT], most = 0, least = INT32_MAX;
     float m[RT], l[RT];
-    int most = 0;
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
-        const int r = r0 + 16 * i + n;
-        load_operand<D, TQ>(q[i], query_row(a, x, min(r, a.M - 1)), g);
-        lim[i] = limit_of(a, x, r);
+        const Query r(a, r0 + 16 * i + n);
+        query_operand<D, TQ>(q[i], a, load_words<D, TQ>(r.row(a, x), g));
+        lim[i] = r.limit(a, x);
         most = max(most, lim[i]);
+        least = min(least, r.real ? lim[i] : INT32_MAX);
         m[i] = -INFINITY;
         l[i] = 0.f;
     }
-#pragma unroll
-    for (int off = 8; off > 0; off >>= 1) most = max(most, __shfl_xor(most, off));
-    k1 = min(k1, __builtin_amdgcn_readfirstlane(most));
+    const int k1 = min(min(k0 + each, x.len), wave_max(most));
+    least = min(wave_min(least), k1);
     const char *Kh = a.K + x.b * a.sk.batch + x.h * a.sk.head;
-    for (int j0 = k0; j0 < k1; j0 += 64) {
-        f32x4 t[4][RT];
-        const float c = tile_scale<TK>(a, bh, j0);
+    auto load = [&](int j) { return load_words<D, TK>(Kh + (int64_t)min(j + n, x.len - 1) * a.sk.seq, g); };
+    if (k0 < k1) {
+        Words<D, TK> ahead[PF];
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-            Operand<D, TK> k;
-            load_operand<D, TK>(k, Kh + (int64_t)min(j0 + 16 * kt + n, x.len - 1) * a.sk.seq, g);
+        for (int i = 0; i < PF; ++i) ahead[i] = load(k0 + 16 * i);
+        for (int j0 = k0; j0 < k1; j0 += 64) {
+            f32x4 t[4][RT];
+            const float c = tile_scale<TK>(a, bh, j0);
 #pragma unroll
-            for (int i = 0; i < RT; ++i) t[kt][i] = logits<D, TK, TQ>(k, q[i]);
-        }
+            for (int kt = 0; kt < 4; ++kt) {
+                Operand<D, TK> k;
+                make_operand<D, TK>(k, ahead[kt % PF]);
+                ahead[kt % PF] = load(j0 + 16 * (kt + PF));
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            float top = m[i];
+                for (int i = 0; i < RT; ++i) t[kt][i] = logits<D, TK, TQ>(k, q[i]);
+            }
+            const bool masked = j0 + 64 > least;          // (scalar)
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
+            for (int i = 0; i < RT; ++i) {
+                float top = -INFINITY;
+                if (masked) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int key = j0 + 16 * kt + 4 * g + e;
-                    t[kt][i][e] = key < min(lim[i], k1) ? c * t[kt][i][e] : -INFINITY;
-                    top = fmaxf(top, t[kt][i][e]);
+                    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const bool seen = j0 + 16 * kt + 4 * g + e < min(lim[i], k1);
+                            const float v = c * t[kt][i][e];
+                            t[kt][i][e] = seen ? v : -INFINITY;
+                            top = fmaxf(top, t[kt][i][e]);
+                        }
+                } else {
+#pragma unroll
+                    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                        for (int e = 0; e < 4; e += 2) top = fmaxf(fmaxf(t[kt][i][e], t[kt][i][e + 1]), top);
+                    top *= c;
                 }
-            const float ref = top == -INFINITY ? 0.f : top;
-            float s = l[i] * __builtin_amdgcn_exp2f(m[i] - ref);
+                top = fmaxf(m[i], top);
+                const float ref = top == -INFINITY ? 0.f : top, cc = masked ? 1.f : c;
+                float s = l[i] * __builtin_amdgcn_exp2f(m[i] - ref);
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
+                for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f(t[kt][i][e] - ref);
-            l[i] = s;
-            m[i] = top;
-            if (!ROWS && a.logits != nullptr && r0 + 16 * i + n < a.M) {
-                float *row = a.logits + ((size_t)bh * a.M + r0 + 16 * i + n) * a.pitch + j0 + 4 * g;
+                    for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f(fmaf(cc, t[kt][i][e], -ref));
+                l[i] = s;
+                m[i] = top;
+                if (!ROWS && a.logits != nullptr && r0 + 16 * i + n < a.M) {
+                    float *row = a.logits + ((size_t)bh * a.M + r0 + 16 * i + n) * a.pitch + j0 + 4 * g;
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt) *reinterpret_cast<f32x4 *>(row + 16 * kt) = t[kt][i];
+                    for (int kt = 0; kt < 4; ++kt) *reinterpret_cast<f32x4 *>(row + 16 * kt) = masked ? t[kt][i] : c * t[kt][i];
+                }
             }
         }
     }
@@ -224,10 +298,10 @@ __global__ __launch_bounds__(NT) void stats_kernel(ScoresArgs a)
         join(m[i], l[i], __shfl_xor(m[i], 32), __shfl_xor(l[i], 32));
         const int r = r0 + 16 * i + n;
         if (g == 0 && r < a.M) {
-            if (ROWS) {
-                a.stats[(size_t)bh * a.M + r] = l[i] == 0.f ? INFINITY : m[i] + __builtin_amdgcn_logf(l[i]);
+            if (ROWS && a.splits == 1) {
+                a.lse[(size_t)bh * a.M + r] = l[i] == 0.f ? INFINITY : m[i] + __builtin_amdgcn_logf(l[i]);
             } else {
-                const size_t at = ((size_t)bh * a.splits + blockIdx.x * NW + wave) * a.M + r;
+                const size_t at = ((size_t)bh * a.splits + part) * a.M + r;
                 a.stats[2 * at] = m[i];
                 a.stats[2 * at + 1] = l[i];
             }
@@ -235,13 +309,11 @@ __global__ __launch_bounds__(NT) void stats_kernel(ScoresArgs a)
     }
 }
 
-constexpr int FEW = 64;                                   // queries at most whose keys are cut into parts
+constexpr int FEW = 64;                                   // queries at most that a workgroup's waves share in the statistics
 
-// log2 of the sums of weights of a head's few queries, from its parts
-__device__ __forceinline__ void merge_stats(const ScoresArgs &a, int bh, float (&lse)[FEW])
+// log2 of the sum of weights of query r, from its parts; by four neighbouring threads
+__device__ __forceinline__ float merged(const ScoresArgs &a, int bh, int r, int sub)
 {
-    // four threads per query, each every fourth part
-    const int r = threadIdx.x / 4, sub = threadIdx.x % 4;
     float m = -INFINITY, l = 0.f;
     if (r < a.M)
         for (int s = sub; s < a.splits; s += 4) {
@@ -250,8 +322,22 @@ __device__ __forceinline__ void merge_stats(const ScoresArgs &a, int bh, float (
         }
     join(m, l, __shfl_xor(m, 1), __shfl_xor(l, 1));
     join(m, l, __shfl_xor(m, 2), __shfl_xor(l, 2));
-    if (sub == 0 && r < a.M) lse[r] = l == 0.f ? INFINITY : m + __builtin_amdgcn_logf(l);
+    return l == 0.f ? INFINITY : m + __builtin_amdgcn_logf(l);
+}
+
+// of a head's few queries, in LDS
+__device__ __forceinline__ void merge_few(const ScoresArgs &a, int bh, float (&lse)[FEW])
+{
+    const float v = merged(a, bh, threadIdx.x / 4, threadIdx.x % 4);
+    if (threadIdx.x % 4 == 0) lse[threadIdx.x / 4] = v;
     __syncthreads();
+}
+
+__global__ __launch_bounds__(NT) void merge_stats_kernel(ScoresArgs a)
+{
+    const int r = blockIdx.x * (NT / 4) + threadIdx.x / 4;
+    const float v = merged(a, blockIdx.y, r, threadIdx.x % 4);
+    if (threadIdx.x % 4 == 0 && r < a.M) a.lse[(size_t)blockIdx.y * a.M + r] = v;
 }
 
 // Shares from stored logits: four keys per thread
@@ -260,7 +346,7 @@ __global__ __launch_bounds__(NT) void stored_shares_kernel(ScoresArgs a)
     __shared__ float lse[FEW];
     const int bh = blockIdx.y, len = cache_length(a.seqlens, bh / a.HC, a.L_max), j = (blockIdx.x * NT + threadIdx.x) * 4;
     if ((int)blockIdx.x * NT * 4 >= len) return;
-    merge_stats(a, bh, lse);
+    merge_few(a, bh, lse);
     if (j >= len) return;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     for (int r = 0; r < a.M; ++r) {
@@ -276,7 +362,7 @@ __global__ __launch_bounds__(NT) void stored_shares_kernel(ScoresArgs a)
         if (j + e < len) out[e] += s[e];
 }
 
-// Shares of 64 keys per workgroup, whose waves take every fourth tile of the queries; summed in a fixed order
+// Shares of 64 keys per workgroup, whose waves take every fourth tile of the queries (the next one on its way); summed in a fixed order
 template <int D, typename TK, typename TQ>
 __global__ __launch_bounds__(NT) void shares_kernel(ScoresArgs a)
 {
@@ -286,28 +372,44 @@ __global__ __launch_bounds__(NT) void shares_kernel(ScoresArgs a)
     const int bh = blockIdx.y, j0 = blockIdx.x * 64;
     const Head x = head_of(a, bh);
     if (j0 >= x.len) return;
-    if (a.splits > 0) merge_stats(a, bh, lse);
+    const bool few = a.lse == nullptr;
+    if (few) merge_few(a, bh, lse);
     const char *Kh = a.K + x.b * a.sk.batch + x.h * a.sk.head;
     Operand<D, TK> k[4];
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt) load_operand<D, TK>(k[kt], Kh + (int64_t)min(j0 + 16 * kt + n, x.len - 1) * a.sk.seq, g);
+    for (int kt = 0; kt < 4; ++kt) make_operand<D, TK>(k[kt], load_words<D, TK>(Kh + (int64_t)min(j0 + 16 * kt + n, x.len - 1) * a.sk.seq, g));
     const float c = tile_scale<TK>(a, bh, j0);
     f32x4 s[4];
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) s[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int r0 = 16 * wave; r0 < a.M; r0 += 16 * NW) {
-        const int r = r0 + n, lim = limit_of(a, x, r);
-        if (__builtin_amdgcn_ballot_w64(lim > j0) == 0) continue;
+    // One query head: those in front of the block's first key see none of it
+    const int start = a.group == 1 ? max(0, j0 - (x.len - a.nq)) / (16 * NW) * (16 * NW) : 0;
+    struct Tile { Words<D, TQ> q; float ref; int lim; };
+    auto load = [&](int r0) {
+        Tile t;
+        const Query r(a, r0 + n);
+        t.q = load_words<D, TQ>(r.row(a, x), g);
+        const int at = min(r0 + n, a.M - 1);
+        t.ref = few ? lse[at & (FEW - 1)] : a.lse[(size_t)bh * a.M + at];
+        t.lim = r.limit(a, x);
+        return t;
+    };
+    Tile next = load(start + 16 * wave);
+    for (int r0 = start + 16 * wave; r0 < a.M; r0 += 16 * NW) {
+        const Tile now = next;
+        next = load(r0 + 16 * NW);
+        if (__builtin_amdgcn_ballot_w64(now.lim > j0) == 0) continue;
         Operand<D, TQ> q;
-        load_operand<D, TQ>(q, query_row(a, x, min(r, a.M - 1)), g);
-        const float ref = r >= a.M ? INFINITY : a.splits > 0 ? lse[r] : a.stats[(size_t)bh * a.M + r];
+        query_operand<D, TQ>(q, a, now.q);
+        const bool whole = __builtin_amdgcn_ballot_w64(now.lim < j0 + 64) == 0;
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
             const f32x4 t = logits<D, TK, TQ>(k[kt], q);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(c, t[e], -ref));
-                s[kt][e] += j0 + 16 * kt + 4 * g + e < lim ? p : 0.f;
+                float p = __builtin_amdgcn_exp2f(fmaf(c, t[e], -now.ref));
+                if (!whole) p = j0 + 16 * kt + 4 * g + e < now.lim ? p : 0.f;
+                s[kt][e] += p;
             }
         }
     }
@@ -323,15 +425,15 @@ __global__ __launch_bounds__(NT) void shares_kernel(ScoresArgs a)
     if (j < 64 && j0 + j < x.len) a.scores[(size_t)bh * a.L_max + j0 + j] += (part[0][j] + part[1][j]) + (part[2][j] + part[3][j]);
 }
 
-// How a call is cut
+// How a call is cut.  A wave's queries: 16 RT (fp32 queries are three operands each: two tiles of 16, otherwise four)
 struct ScoresPlan {
-    int M, splits;             // splits == 0: the waves have queries of their own
+    int M, splits, blocks;     // blocks == 0: a workgroup's waves share the queries
     bool stored;
     int64_t pitch;
-    size_t stats_bytes, bytes;
+    size_t stats_bytes, lse_bytes, bytes;
 };
 
-ScoresPlan scores_plan(const llla_cache &c, int H, int nq)
+ScoresPlan scores_plan(const llla_cache &c, int H, int nq, llla_dtype in)
 {
     ScoresPlan p{};
     p.M = H / c.H * nq;
@@ -342,10 +444,16 @@ ScoresPlan scores_plan(const llla_cache &c, int H, int nq)
         p.splits = NW * wgs;
         // a logit is written and read, a row of the cache would be read a second time
         p.stored = 8 * p.M <= c.d * size;
+    } else {
+        const int rows = 16 * (in == LLLA_F32 ? 2 : 4) * NW;
+        p.blocks = (p.M + rows - 1) / rows;
+        // parts of the keys, of at least 128, while there are fewer workgroups than compute units
+        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / ((int64_t)heads * p.blocks), (c.L_max + 127) / 128));
     }
     p.pitch = p.stored ? (int64_t)(c.L_max + 63) / 64 * 64 : 0;
-    p.stats_bytes = round_up((size_t)heads * p.M * (p.splits ? 2 * p.splits : 1) * sizeof(float), 256);
-    p.bytes = p.stats_bytes + round_up((size_t)heads * p.M * p.pitch * sizeof(float), 256);
+    p.stats_bytes = p.blocks && p.splits == 1 ? 0 : round_up((size_t)heads * p.M * 2 * p.splits * sizeof(float), 256);
+    p.lse_bytes = p.blocks ? round_up((size_t)heads * p.M * sizeof(float), 256) : 0;
+    p.bytes = p.stats_bytes + p.lse_bytes + round_up((size_t)heads * p.M * p.pitch * sizeof(float), 256);
     return p;
 }
 
@@ -353,7 +461,7 @@ template <int D, typename TK, typename TQ>
 hipError_t launch_scores(const ScoresProblem &p)
 {
     const llla_cache &c = p.c;
-    const ScoresPlan plan = scores_plan(c, p.H, p.nq);
+    const ScoresPlan plan = scores_plan(c, p.H, p.nq, p.in);
     constexpr int KS = RowType<TK>::SIZE, QS = RowType<TQ>::SIZE, RT = QS == 4 ? 2 : 4;
     ScoresArgs a{};
     a.Q = static_cast<const char *>(p.Q);
@@ -365,19 +473,23 @@ hipError_t launch_scores(const ScoresProblem &p)
     a.seqlens = p.seqlens;
     a.HC = c.H; a.group = p.H / c.H; a.nq = p.nq; a.M = plan.M; a.L_max = c.L_max;
     a.splits = plan.splits;
-    a.cscale = p.scale * LOG2E;
-    a.stats = static_cast<float *>(p.ws);
-    a.logits = plan.stored ? reinterpret_cast<float *>(static_cast<char *>(p.ws) + plan.stats_bytes) : nullptr;
+    a.blocks = plan.blocks;
+    a.cscale = (p.scale < 0.f ? -p.scale : p.scale) * LOG2E;
+    a.negative = p.scale < 0.f ? 1 : 0;
+    char *ws = static_cast<char *>(p.ws);
+    a.stats = reinterpret_cast<float *>(ws);
+    a.lse = plan.blocks ? reinterpret_cast<float *>(ws + plan.stats_bytes) : nullptr;
+    a.logits = plan.stored ? reinterpret_cast<float *>(ws + plan.stats_bytes + plan.lse_bytes) : nullptr;
     a.pitch = plan.pitch;
     const int heads = c.B * c.H;
-    if (plan.splits > 0) {
+    if (!plan.blocks) {
         const dim3 grid(plan.splits / NW, heads);
         if (plan.M <= 16) hipLaunchKernelGGL((stats_kernel<D, TK, TQ, 1, false>), grid, dim3(NT), 0, p.stream, a);
         else if (plan.M <= 32) hipLaunchKernelGGL((stats_kernel<D, TK, TQ, 2, false>), grid, dim3(NT), 0, p.stream, a);
         else hipLaunchKernelGGL((stats_kernel<D, TK, TQ, 4, false>), grid, dim3(NT), 0, p.stream, a);
     } else {
-        const int rows = 16 * RT * NW;
-        hipLaunchKernelGGL((stats_kernel<D, TK, TQ, RT, true>), dim3((plan.M + rows - 1) / rows, heads), dim3(NT), 0, p.stream, a);
+        hipLaunchKernelGGL((stats_kernel<D, TK, TQ, RT, true>), dim3(plan.blocks * plan.splits, heads), dim3(NT), 0, p.stream, a);
+        if (plan.splits > 1) hipLaunchKernelGGL(merge_stats_kernel, dim3((plan.M + NT / 4 - 1) / (NT / 4), heads), dim3(NT), 0, p.stream, a);
     }
     if (plan.stored) hipLaunchKernelGGL(stored_shares_kernel, dim3((c.L_max + 4 * NT - 1) / (4 * NT), heads), dim3(NT), 0, p.stream, a);
     else hipLaunchKernelGGL((shares_kernel<D, TK, TQ>), dim3((c.L_max + 63) / 64, heads), dim3(NT), 0, p.stream, a);
@@ -398,7 +510,7 @@ hipError_t scores_by_type(const ScoresProblem &p)
 
 }  // namespace
 
-size_t cache_scores_workspace_bytes(const llla_cache &c, int H, int nq, llla_dtype) { return scores_plan(c, H, nq).bytes; }
+size_t cache_scores_workspace_bytes(const llla_cache &c, int H, int nq, llla_dtype in) { return scores_plan(c, H, nq, in).bytes; }
 
 hipError_t cache_scores(const ScoresProblem &p)
 {

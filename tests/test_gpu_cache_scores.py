@@ -82,6 +82,26 @@ def test_peaked_weights_and_accumulation(dtype):
     _check(cache, Q, scale, [700], once, "second")
 
 
+@pytest.mark.parametrize("scale", [-0.3, 0.0])
+@pytest.mark.parametrize("nq", [1, 90])
+def test_scales_that_are_not_positive(scale, nq):
+    for dtype, q_dtype in ((E4M3, BF16), (BF16, BF16), (F32, F32)):
+        cache, Q = _case(2, 4, 2, 333, 32, dtype, nq, q_dtype, 3)
+        before = cache.scores.clone()
+        llla.llla_cache_scores(Q, cache, scale, seqlens=torch.tensor([333, 100], dtype=torch.int32, device=DEV))
+        _check(cache, Q, scale, [333, 100], before, "scale %g nq=%d" % (scale, nq))
+
+
+@pytest.mark.parametrize("dtype,q_dtype,H,HC,nq,L", [(F32, F32, 16, 4, 40, 2999), (BF16, BF16, 6, 2, 100, 1500), (I8, F32, 8, 8, 300, 700), (E4M3, BF16, 2, 1, 129, 4000)])
+def test_many_queries_of_few_heads(dtype, q_dtype, H, HC, nq, L):
+    """More queries than a workgroup's waves share, keys cut into parts; groups of query heads, lengths of their own."""
+    cache, Q = _case(2, H, HC, L, 64, dtype, nq, q_dtype, nq)
+    lens = [L, L // 3]
+    before = cache.scores.clone()
+    llla.llla_cache_scores(Q, cache, 0.125, seqlens=torch.tensor(lens, dtype=torch.int32, device=DEV))
+    _check(cache, Q, 0.125, lens, before, "many")
+
+
 def test_sums_to_the_number_of_queries():
     cache, Q = _case(2, 4, 4, 3000, 64, BF16, 3000, BF16, 6)
     cache.scores.zero_()
