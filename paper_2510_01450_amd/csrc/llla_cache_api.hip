@@ -32,7 +32,7 @@ llla_status check_cache(const llla_cache *c, bool values)
     if (!number_type(c->type) && !codes(c->type)) return LLLA_ERR_DTYPE;
     if (!dim_ok(c->d)) return LLLA_ERR_UNSUPPORTED;
     if (codes(c->type) && (!c->k_exp || (values && !c->v_exp))) return LLLA_ERR_NULL;
-    if ((int64_t)c->B * c->H > 65535 || c->L_max > 2147483647 - 64) return LLLA_ERR_SHAPE;
+    if ((int64_t)c->B * c->H > 65535 || c->L_max > (1 << 30)) return LLLA_ERR_SHAPE;
     if (!strides_cover(c->sk, c->B, c->H, c->L_max, c->d) || (values && !strides_cover(c->sv, c->B, c->H, c->L_max, c->d))) return LLLA_ERR_SHAPE;
     if (c->sk.seq >= MAX_ROW_STRIDE || (values && c->sv.seq >= MAX_ROW_STRIDE)) return LLLA_ERR_SHAPE;
     if (!aligned(c->K, 16) || !strides_aligned(c->sk, c->type) || (values && (!aligned(c->V, 16) || !strides_aligned(c->sv, c->type))) ||

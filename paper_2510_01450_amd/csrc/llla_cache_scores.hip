@@ -193,6 +193,13 @@ __device__ __forceinline__ void join(float &m, float &l, float m2, float l2)
     m = top;
 }
 
+// 256 registers for a wave (matrix results then stay where vector instructions read them), or all 512 where operands of three terms need them
+template <int D, typename TK, typename TQ, int RT>
+struct RegisterFile {
+    static constexpr int NEED = D / 32 * 4 * (RT * RowType<TQ>::TERMS + 4 * RowType<TK>::TERMS);
+    static constexpr int WAVES = NEED > 128 ? 1 : 2;
+};
+
 __device__ __forceinline__ int wave_min(int x)
 {
 #pragma unroll
@@ -208,17 +215,20 @@ __device__ __forceinline__ int wave_max(int x)
 
 // Statistics of 16 RT queries per wave.  ROWS: the waves of a workgroup have queries of their own and walk through the same keys; otherwise
 // they share the queries and have parts of the keys.
-// Per logit one fused multiply-add, one exponential and one addition, and half a maximum; masks only in blocks that some query does not see whole.  Rows are
-// requested PF tiles of 16 keys ahead.
+// Per logit one fused multiply-add, one exponential and one addition.  A sum of weights relative to any logit of its keys is as good as one
+// relative to the largest while it stays below FAR: the reference is the first block's largest, and is raised by the block that passes FAR.
+// Masks only in blocks that some query does not see whole.  Rows are requested PF tiles of 16 keys ahead.
+constexpr float FAR = 0x1p64f;
+
 template <int D, typename TK, typename TQ, int RT, bool ROWS>
-__global__ __launch_bounds__(NT) void stats_kernel(ScoresArgs a)
+__global__ __launch_bounds__(NT, (RegisterFile<D, TK, TQ, RT>::WAVES)) void stats_kernel(ScoresArgs a)
 {
     constexpr int PF = Words<D, TK>::BYTES > 32 ? 1 : 4;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16, n = lane % 16;
     const int bh = blockIdx.y;
     const Head x = head_of(a, bh);
-    // (the last queries see most: first)
-    const int r0 = ROWS ? ((a.blocks - 1 - (int)blockIdx.x % a.blocks) * NW + wave) * 16 * RT : 0, part = ROWS ? (int)blockIdx.x / a.blocks : (int)blockIdx.x * NW + wave;
+    // (every XCD takes each eighth workgroup: turned by the head, or some would have the queries that see most and others those that see least)
+    const int r0 = ROWS ? ((int)((blockIdx.x + blockIdx.y) % a.blocks) * NW + wave) * 16 * RT : 0, part = ROWS ? (int)blockIdx.x / a.blocks : (int)blockIdx.x * NW + wave;
     if (r0 >= a.M) return;
     const int each = ((x.len + a.splits - 1) / a.splits + 63) & ~63;
     const int k0 = (int)min((int64_t)part * each, (int64_t)x.len);
@@ -255,39 +265,60 @@ __global__ __launch_bounds__(NT) void stats_kernel(ScoresArgs a)
                 for (int i = 0; i < RT; ++i) t[kt][i] = logits<D, TK, TQ>(k, q[i]);
             }
             const bool masked = j0 + 64 > least;          // (scalar)
+            if (masked) {
 #pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                float top = -INFINITY;
-                if (masked) {
+                for (int i = 0; i < RT; ++i)
 #pragma unroll
                     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const bool seen = j0 + 16 * kt + 4 * g + e < min(lim[i], k1);
-                            const float v = c * t[kt][i][e];
-                            t[kt][i][e] = seen ? v : -INFINITY;
-                            top = fmaxf(top, t[kt][i][e]);
-                        }
-                } else {
+                        for (int e = 0; e < 4; ++e) t[kt][i][e] = j0 + 16 * kt + 4 * g + e < min(lim[i], k1) ? c * t[kt][i][e] : -INFINITY;
+            }
+            const float cc = masked ? 1.f : c;
+            float sum[RT];
+            bool far = j0 == k0;
+            if (!far) {
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    const float ref = m[i];
+                    float s = 0.f;
+#pragma unroll
+                    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f(fmaf(cc, t[kt][i][e], -ref));
+                    sum[i] = s;
+                    far = far || !(s < FAR);
+                }
+                far = __builtin_amdgcn_ballot_w64(far) != 0;
+            }
+            if (far) {
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    float top = -INFINITY;
 #pragma unroll
                     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
                         for (int e = 0; e < 4; e += 2) top = fmaxf(fmaxf(t[kt][i][e], t[kt][i][e + 1]), top);
-                    top *= c;
+                    top = fmaxf(m[i], cc * top);
+                    const float ref = top == -INFINITY ? 0.f : top;
+                    float s = 0.f;
+#pragma unroll
+                    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f(fmaf(cc, t[kt][i][e], -ref));
+                    l[i] = l[i] * __builtin_amdgcn_exp2f(m[i] - ref) + s;
+                    m[i] = top;
                 }
-                top = fmaxf(m[i], top);
-                const float ref = top == -INFINITY ? 0.f : top, cc = masked ? 1.f : c;
-                float s = l[i] * __builtin_amdgcn_exp2f(m[i] - ref);
+            } else {
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
+                for (int i = 0; i < RT; ++i) l[i] += sum[i];
+            }
+            if (!ROWS && a.logits != nullptr) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f(fmaf(cc, t[kt][i][e], -ref));
-                l[i] = s;
-                m[i] = top;
-                if (!ROWS && a.logits != nullptr && r0 + 16 * i + n < a.M) {
+                for (int i = 0; i < RT; ++i) {
+                    if (r0 + 16 * i + n >= a.M) continue;
                     float *row = a.logits + ((size_t)bh * a.M + r0 + 16 * i + n) * a.pitch + j0 + 4 * g;
 #pragma unroll
-                    for (int kt = 0; kt < 4; ++kt) *reinterpret_cast<f32x4 *>(row + 16 * kt) = masked ? t[kt][i] : c * t[kt][i];
+                    for (int kt = 0; kt < 4; ++kt) *reinterpret_cast<f32x4 *>(row + 16 * kt) = cc * t[kt][i];
                 }
             }
         }
@@ -364,12 +395,12 @@ __global__ __launch_bounds__(NT) void stored_shares_kernel(ScoresArgs a)
 
 // Shares of 64 keys per workgroup, whose waves take every fourth tile of the queries (the next one on its way); summed in a fixed order
 template <int D, typename TK, typename TQ>
-__global__ __launch_bounds__(NT) void shares_kernel(ScoresArgs a)
+__global__ __launch_bounds__(NT, (RegisterFile<D, TK, TQ, 4>::WAVES)) void shares_kernel(ScoresArgs a)
 {
     __shared__ float lse[FEW];
     __shared__ float part[NW][64];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16, n = lane % 16;
-    const int bh = blockIdx.y, j0 = blockIdx.x * 64;
+    const int bh = blockIdx.y, j0 = (int)((blockIdx.x + blockIdx.y) % gridDim.x) * 64;   // (turned by the head, as above)
     const Head x = head_of(a, bh);
     if (j0 >= x.len) return;
     const bool few = a.lse == nullptr;
@@ -384,14 +415,23 @@ __global__ __launch_bounds__(NT) void shares_kernel(ScoresArgs a)
     for (int kt = 0; kt < 4; ++kt) s[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
     // One query head: those in front of the block's first key see none of it
     const int start = a.group == 1 ? max(0, j0 - (x.len - a.nq)) / (16 * NW) * (16 * NW) : 0;
+    // A lane's query, 16 NW further each time without a division
+    Query r(a, start + 16 * wave + n);
+    const char *row = r.row(a, x);
+    const int heads = 16 * NW / a.nq, rest = 16 * NW % a.nq;
+    const int64_t ahead = heads * a.sq.head + rest * a.sq.seq, wrap = a.sq.head - a.nq * a.sq.seq;
     struct Tile { Words<D, TQ> q; float ref; int lim; };
     auto load = [&](int r0) {
         Tile t;
-        const Query r(a, r0 + n);
-        t.q = load_words<D, TQ>(r.row(a, x), g);
         const int at = min(r0 + n, a.M - 1);
+        t.q = load_words<D, TQ>(row, g);
         t.ref = few ? lse[at & (FEW - 1)] : a.lse[(size_t)bh * a.M + at];
         t.lim = r.limit(a, x);
+        r.i += rest;
+        const bool over = r.i >= a.nq;
+        r.i -= over ? a.nq : 0;
+        r.real = r0 + 16 * NW + n < a.M;
+        row += r.real ? ahead + (over ? wrap : 0) : 0;
         return t;
     };
     Tile next = load(start + 16 * wave);
@@ -401,16 +441,22 @@ __global__ __launch_bounds__(NT) void shares_kernel(ScoresArgs a)
         if (__builtin_amdgcn_ballot_w64(now.lim > j0) == 0) continue;
         Operand<D, TQ> q;
         query_operand<D, TQ>(q, a, now.q);
-        const bool whole = __builtin_amdgcn_ballot_w64(now.lim < j0 + 64) == 0;
+        f32x4 t[4];
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-            const f32x4 t = logits<D, TK, TQ>(k[kt], q);
+        for (int kt = 0; kt < 4; ++kt) t[kt] = logits<D, TK, TQ>(k[kt], q);
+        if (__builtin_amdgcn_ballot_w64(now.lim < j0 + 64) == 0) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float p = __builtin_amdgcn_exp2f(fmaf(c, t[e], -now.ref));
-                if (!whole) p = j0 + 16 * kt + 4 * g + e < now.lim ? p : 0.f;
-                s[kt][e] += p;
-            }
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[kt][e] += __builtin_amdgcn_exp2f(fmaf(c, t[kt][e], -now.ref));
+        } else {
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(c, t[kt][e], -now.ref));
+                    s[kt][e] += j0 + 16 * kt + 4 * g + e < now.lim ? p : 0.f;
+                }
         }
     }
 #pragma unroll
@@ -447,8 +493,10 @@ ScoresPlan scores_plan(const llla_cache &c, int H, int nq, llla_dtype in)
     } else {
         const int rows = 16 * (in == LLLA_F32 ? 2 : 4) * NW;
         p.blocks = (p.M + rows - 1) / rows;
-        // parts of the keys, of at least 128, while there are fewer workgroups than compute units
-        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / ((int64_t)heads * p.blocks), (c.L_max + 127) / 128));
+        // parts of the keys, for sixteen workgroups per compute unit (queries of a prompt see few keys or many, and four are resident), but
+        // of at least 512 keys, or 128 while there are fewer workgroups than compute units
+        const int64_t each = (int64_t)heads * p.blocks;
+        p.splits = (int)std::max<int64_t>({1, std::min<int64_t>(4096 / each, (c.L_max + 511) / 512), std::min<int64_t>(512 / each, (c.L_max + 127) / 128)});
     }
     p.pitch = p.stored ? (int64_t)(c.L_max + 63) / 64 * 64 : 0;
     p.stats_bytes = p.blocks && p.splits == 1 ? 0 : round_up((size_t)heads * p.M * 2 * p.splits * sizeof(float), 256);
