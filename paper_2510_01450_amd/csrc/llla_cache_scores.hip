@@ -40,22 +40,19 @@ struct Words {
     unsigned w[BYTES / 4];
 };
 
-template <int D, typename T>
+// ONCE: not to be kept in the caches
+template <int D, typename T, bool ONCE = false>
 __device__ __forceinline__ Words<D, T> load_words(const char *row, int g)
 {
-    constexpr int BYTES = Words<D, T>::BYTES;
+    constexpr int BYTES = Words<D, T>::BYTES, N = BYTES < 16 ? BYTES / 4 : 4;
+    typedef unsigned part __attribute__((ext_vector_type(N)));
     Words<D, T> o;
-    const char *p = row + g * BYTES;
-    if constexpr (BYTES == 4) o.w[0] = *reinterpret_cast<const unsigned *>(p);
-    else if constexpr (BYTES == 8) {
-        const uint2 v = *reinterpret_cast<const uint2 *>(p);
-        o.w[0] = v.x; o.w[1] = v.y;
-    } else {
+    const part *p = reinterpret_cast<const part *>(row + g * BYTES);
 #pragma unroll
-        for (int i = 0; i < BYTES / 16; ++i) {
-            const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
-            o.w[4 * i] = v.x; o.w[4 * i + 1] = v.y; o.w[4 * i + 2] = v.z; o.w[4 * i + 3] = v.w;
-        }
+    for (int i = 0; i < BYTES / 4 / N; ++i) {
+        const part v = ONCE ? __builtin_nontemporal_load(p + i) : p[i];
+#pragma unroll
+        for (int e = 0; e < N; ++e) o.w[N * i + e] = v[e];
     }
     return o;
 }
@@ -248,7 +245,7 @@ __global__ __launch_bounds__(NT, (RegisterFile<D, TK, TQ, RT>::WAVES)) void stat
     const int k1 = min(min(k0 + each, x.len), wave_max(most));
     least = min(wave_min(least), k1);
     const char *Kh = a.K + x.b * a.sk.batch + x.h * a.sk.head;
-    auto load = [&](int j) { return load_words<D, TK>(Kh + (int64_t)min(j + n, x.len - 1) * a.sk.seq, g); };
+    auto load = [&](int j) { return load_words<D, TK, !ROWS && RT == 1>(Kh + (int64_t)min(j + n, x.len - 1) * a.sk.seq, g); };
     if (k0 < k1) {
         Words<D, TK> ahead[PF];
 #pragma unroll
@@ -377,20 +374,26 @@ __global__ __launch_bounds__(NT) void stored_shares_kernel(ScoresArgs a)
     __shared__ float lse[FEW];
     const int bh = blockIdx.y, len = cache_length(a.seqlens, bh / a.HC, a.L_max), j = (blockIdx.x * NT + threadIdx.x) * 4;
     if ((int)blockIdx.x * NT * 4 >= len) return;
+    const float *row = a.logits + (size_t)bh * a.M * a.pitch + min(j, ((len + 63) & ~63) - 4);
+    float *out = a.scores + (size_t)bh * a.L_max + j;
+    const bool wide = (a.L_max & 3) == 0 && (reinterpret_cast<uintptr_t>(a.scores) & 15) == 0 && j + 4 <= len;
+    f32x4 next = *reinterpret_cast<const f32x4 *>(row), s = {0.f, 0.f, 0.f, 0.f}, old = s;
+    if (wide) old = *reinterpret_cast<const f32x4 *>(out);
     merge_few(a, bh, lse);
     if (j >= len) return;
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
     for (int r = 0; r < a.M; ++r) {
         // (keys behind the last one that any query sees have no logits)
         const int lim = min(len, len - a.nq + r % a.nq + 1);
-        const f32x4 t = *reinterpret_cast<const f32x4 *>(a.logits + ((size_t)bh * a.M + r) * a.pitch + j);
+        const f32x4 t = next;
+        if (r + 1 < a.M) next = *reinterpret_cast<const f32x4 *>(row += a.pitch);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[e] += j + e < lim ? __builtin_amdgcn_exp2f(t[e] - lse[r]) : 0.f;
     }
-    float *out = a.scores + (size_t)bh * a.L_max + j;
+    if (wide) *reinterpret_cast<f32x4 *>(out) = old + s;
+    else
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (j + e < len) out[e] += s[e];
+        for (int e = 0; e < 4; ++e)
+            if (j + e < len) out[e] += s[e];
 }
 
 // Shares of 64 keys per workgroup, whose waves take every fourth tile of the queries (the next one on its way); summed in a fixed order
