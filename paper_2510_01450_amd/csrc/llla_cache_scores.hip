@@ -488,8 +488,9 @@ ScoresPlan scores_plan(const llla_cache &c, int H, int nq, llla_dtype in)
     p.M = H / c.H * nq;
     const int heads = c.B * c.H, size = c.type == LLLA_F32 ? 4 : c.type == LLLA_BF16 ? 2 : 1;
     if (p.M <= FEW) {
-        // enough workgroups for the GPU, each wave with at least 256 keys
-        const int wgs = std::max(1, std::min((2048 + heads - 1) / heads, (c.L_max + 1023) / 1024));
+        // six workgroups per compute unit, all resident (512 heads of 32768 int8 keys: 255 us; four 258, eight, in two turns, 272, and more
+        // leave more parts to merge: 263 with sixteen), each wave with at least 256 keys
+        const int wgs = std::max(1, std::min((1536 + heads - 1) / heads, (c.L_max + 1023) / 1024));
         p.splits = NW * wgs;
         // a logit is written and read, a row of the cache would be read a second time
         p.stored = 8 * p.M <= c.d * size;
