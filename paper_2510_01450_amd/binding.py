@@ -1,4 +1,4 @@
-"""Binding of libllla.so -- argument marshalling only: ctypes, and for the ordinary forms of a forward or decode call a native extension
+"""Binding of libllla.so -- argument marshalling only: ctypes, and for the ordinary forms of a forward, decode or cache call a native extension
 (csrc/host/llla_host.cpp) that does the same with less of the host's time."""
 from __future__ import annotations
 
@@ -126,7 +126,7 @@ class _PythonHost:
     def forward(*args):
         return NotImplemented
 
-    decode = forward
+    decode = cache_append = decode_q8 = cache_scores = forward
 
 
 def _load_host():
@@ -159,7 +159,8 @@ def _entry_points(*tensors):
     L = _load(measure)
     _load_host()
     _entries[measure] = tuple(ctypes.cast(f, ctypes.c_void_p).value for f in (
-        L.llla_forward_ex, L.llla_forward_workspace_bytes, L.llla_decode_path, L.llla_decode_workspace_bytes))
+        L.llla_forward_ex, L.llla_forward_workspace_bytes, L.llla_decode_path, L.llla_decode_workspace_bytes, L.llla_cache_append,
+        L.llla_decode_q8, L.llla_decode_q8_workspace_bytes, L.llla_cache_scores, L.llla_cache_scores_workspace_bytes))
     return _entries[measure]
 
 

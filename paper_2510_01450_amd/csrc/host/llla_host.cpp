@@ -1,4 +1,4 @@
-// The host side of a forward or decode call from Python, natively: reads the tensors, allocates result and scratch with torch's allocator and
+// The host side of a forward, decode or cache call from Python, natively: reads the tensors, allocates result and scratch with torch's allocator and
 // calls the C ABI.  A call of one head x 128 rows is 8 us on the GPU and took the host 11.5 in Python (ctypes alone 2.3, strides, sizes and
 // two allocations the rest); from here such calls follow each other at the GPU's pace, 8.1 us, and a single call ends 5 to 7 us earlier.
 //
@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/Functions.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -237,9 +238,171 @@ PyObject *decode(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     END_HANDLE_TH_ERRORS
 }
 
+// An optional contiguous array of `type` on `device`; its sizes are `want`
+bool array(PyObject *o, at::ScalarType type, at::IntArrayRef want, const at::Device &device, void *&p)
+{
+    p = nullptr;
+    if (o == Py_None) return true;
+    if (!is_tensor(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (t.scalar_type() != type || t.device() != device || t.sizes() != want || !t.is_contiguous()) return false;
+    p = t.data_ptr();
+    return true;
+}
+
+// A Cache (a tuple of K, V, k_exp, v_exp, scores, pos) on the current GPU
+bool cache_of(PyObject *o, llla_cache &c, at::Tensor &K)
+{
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 6 || !is_tensor(PyTuple_GET_ITEM(o, 0)) || !is_tensor(PyTuple_GET_ITEM(o, 1))) return false;
+    K = THPVariable_Unpack(PyTuple_GET_ITEM(o, 0));
+    const at::Tensor &V = THPVariable_Unpack(PyTuple_GET_ITEM(o, 1));
+    if (!K.is_cuda() || V.device() != K.device() || V.scalar_type() != K.scalar_type() || !rows4(K, c.sk) || !rows4(V, c.sv) || V.sizes() != K.sizes()) return false;
+    if (c10::impl::VirtualGuardImpl(K.device().type()).getDevice() != K.device()) return false;
+    const bool codes = K.scalar_type() == at::kChar || K.scalar_type() == at::kFloat8_e4m3fn;
+    if (codes) c.type = K.scalar_type() == at::kChar ? LLLA_I8 : LLLA_E4M3;
+    else if (!dtype_of(K.scalar_type(), c.type)) return false;
+    const int64_t B = K.size(0), H = K.size(1), n = K.size(2), d = K.size(3);
+    if (B > MAX_DIM || H > MAX_DIM || n > MAX_DIM - 63 || d > MAX_DIM) return false;
+    c.B = (int)B; c.H = (int)H; c.L_max = (int)n; c.d = (int)d;
+    c.K = K.data_ptr();
+    c.V = V.data_ptr();
+    void *ke = nullptr, *ve = nullptr, *scores, *pos;
+    if (codes && (!array(PyTuple_GET_ITEM(o, 2), at::kChar, {B, H, (n + 63) / 64}, K.device(), ke) ||
+                  !array(PyTuple_GET_ITEM(o, 3), at::kChar, {B, H, (n + 63) / 64}, K.device(), ve) || ke == nullptr || ve == nullptr))
+        return false;
+    if (!array(PyTuple_GET_ITEM(o, 4), at::kFloat, {B, H, n}, K.device(), scores) || !array(PyTuple_GET_ITEM(o, 5), at::kInt, {B, H, n}, K.device(), pos)) return false;
+    c.k_exp = static_cast<int8_t *>(ke);
+    c.v_exp = static_cast<int8_t *>(ve);
+    c.scores = static_cast<float *>(scores);
+    c.pos = static_cast<int32_t *>(pos);
+    return true;
+}
+
+// cache_append(llla_cache_append, cache, k, v, seqlens, new_lens, first_pos, stream)
+PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    llla_cache c{};
+    at::Tensor K;
+    if (n_args != 8 || !cache_of(a[1], c, K) || !is_tensor(a[2]) || !is_tensor(a[3])) return not_implemented();
+    const at::Tensor &k = THPVariable_Unpack(a[2]), &v = THPVariable_Unpack(a[3]);
+    llla_strides sk, sv;
+    llla_dtype in;
+    if (k.device() != K.device() || v.device() != K.device() || k.scalar_type() != v.scalar_type() || !dtype_of(k.scalar_type(), in) || !rows4(k, sk) || !rows4(v, sv) ||
+        k.sizes() != v.sizes() || k.size(0) != c.B || k.size(1) != c.H || k.size(3) != c.d || k.size(2) > MAX_DIM)
+        return not_implemented();
+    void *lens[3];
+    for (int i = 0; i < 3; ++i)
+        if (!array(a[4 + i], at::kInt, {c.B}, K.device(), lens[i])) return not_implemented();
+    void *stream = stream_of(a[7]);
+    if (PyErr_Occurred()) return nullptr;
+    const auto call = reinterpret_cast<decltype(&llla_cache_append)>(PyLong_AsVoidPtr(a[0]));
+    llla_status st;
+    {
+        WithoutGil released;
+        st = call(&c, k.data_ptr(), v.data_ptr(), sk, sv, (int)k.size(2), in, static_cast<int32_t *>(lens[0]), static_cast<int32_t *>(lens[1]),
+                  static_cast<int32_t *>(lens[2]), stream);
+    }
+    return PyLong_FromLong(st);
+    END_HANDLE_TH_ERRORS
+}
+
+// The caller's scratch of a cache call: None, or a contiguous tensor on the cache's device
+bool given_scratch(PyObject *o, const at::Device &device, const at::Tensor *&t)
+{
+    t = nullptr;
+    if (o == Py_None) return true;
+    if (!is_tensor(o)) return false;
+    t = &THPVariable_Unpack(o);
+    return t->device() == device && t->is_contiguous();
+}
+
+// decode_q8(llla_decode_q8, llla_decode_q8_workspace_bytes, q, cache, lam, scale, seqlens, out_dtype, workspace, out, stream)
+PyObject *decode_q8(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    llla_cache c{};
+    at::Tensor K;
+    if (n_args != 11 || !is_tensor(a[2]) || !cache_of(a[3], c, K)) return not_implemented();
+    const at::Tensor &q = THPVariable_Unpack(a[2]);
+    llla_dtype in, out = LLLA_F32;
+    double lambda, scale;
+    at::ScalarType out_type;
+    void *lens;
+    const at::Tensor *given;
+    if ((c.type != LLLA_I8 && c.type != LLLA_E4M3) || q.device() != K.device() || !dtype_of(q.scalar_type(), in) || q.dim() != 3 || !q.is_contiguous() || q.size(0) != c.B ||
+        q.size(2) != c.d || q.size(1) > MAX_DIM || !number(a[4], lambda) || !number(a[5], scale) || !array(a[6], at::kInt, {c.B}, K.device(), lens) ||
+        !result_type(a[7], out_type) || !given_scratch(a[8], K.device(), given))
+        return not_implemented();
+    at::Tensor o;
+    if (a[9] != Py_None) {
+        if (!is_tensor(a[9])) return not_implemented();
+        o = THPVariable_Unpack(a[9]);
+        if (!dtype_of(o.scalar_type(), out) || o.sizes() != q.sizes() || !o.is_contiguous() || o.device() != K.device()) return not_implemented();
+    }
+    void *stream = stream_of(a[10]);
+    if (PyErr_Occurred()) return nullptr;
+    const auto call = reinterpret_cast<decltype(&llla_decode_q8)>(PyLong_AsVoidPtr(a[0]));
+    const auto size = reinterpret_cast<decltype(&llla_decode_q8_workspace_bytes)>(PyLong_AsVoidPtr(a[1]));
+    const int H = (int)q.size(1);
+    llla_status st;
+    {
+        WithoutGil released;
+        if (!o.defined()) {
+            o = at::empty(q.sizes(), at::TensorOptions().device(q.device()).dtype(out_type));
+            dtype_of(out_type, out);
+        }
+        const Scratch ws = scratch(given, given ? 0 : size(&c, H), K.device());
+        st = call(q.data_ptr(), &c, o.data_ptr(), static_cast<int32_t *>(lens), H, in, out, (float)lambda, (float)scale, ws.ptr, ws.bytes, stream);
+    }
+    if (st != LLLA_OK) return PyLong_FromLong(st);
+    if (a[9] != Py_None) {
+        Py_INCREF(a[9]);
+        return a[9];
+    }
+    return THPVariable_Wrap(o);
+    END_HANDLE_TH_ERRORS
+}
+
+// cache_scores(llla_cache_scores, llla_cache_scores_workspace_bytes, Q, cache, scale, seqlens, workspace, stream)
+PyObject *cache_scores(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    llla_cache c{};
+    at::Tensor K;
+    if (n_args != 8 || !is_tensor(a[2]) || !cache_of(a[3], c, K) || c.scores == nullptr) return not_implemented();
+    const at::Tensor &Q = THPVariable_Unpack(a[2]);
+    llla_dtype in;
+    double scale;
+    void *lens;
+    const at::Tensor *given;
+    const int64_t dims = Q.dim();
+    if ((dims != 3 && dims != 4) || Q.device() != K.device() || !dtype_of(Q.scalar_type(), in) || Q.stride(dims - 1) != 1 || Q.size(0) != c.B || Q.size(dims - 1) != c.d ||
+        Q.size(1) > MAX_DIM || (dims == 4 && Q.size(2) > MAX_DIM) || (c.type != LLLA_I8 && c.type != LLLA_E4M3 && c.type != in) || !number(a[4], scale) ||
+        !array(a[5], at::kInt, {c.B}, K.device(), lens) || !given_scratch(a[6], K.device(), given))
+        return not_implemented();
+    const int H = (int)Q.size(1), nq = dims == 3 ? 1 : (int)Q.size(2);
+    const llla_strides sq{Q.stride(0), Q.stride(1), dims == 3 ? c.d : Q.stride(2)};
+    void *stream = stream_of(a[7]);
+    if (PyErr_Occurred()) return nullptr;
+    const auto call = reinterpret_cast<decltype(&llla_cache_scores)>(PyLong_AsVoidPtr(a[0]));
+    const auto size = reinterpret_cast<decltype(&llla_cache_scores_workspace_bytes)>(PyLong_AsVoidPtr(a[1]));
+    llla_status st;
+    {
+        WithoutGil released;
+        const Scratch ws = scratch(given, given ? 0 : size(&c, H, nq, in), K.device());
+        st = call(Q.data_ptr(), &c, sq, static_cast<int32_t *>(lens), H, nq, in, (float)scale, ws.ptr, ws.bytes, stream);
+    }
+    return PyLong_FromLong(st);
+    END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
     {"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(forward)), METH_FASTCALL, nullptr},
     {"decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(decode)), METH_FASTCALL, nullptr},
+    {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(cache_append)), METH_FASTCALL, nullptr},
+    {"decode_q8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(decode_q8)), METH_FASTCALL, nullptr},
+    {"cache_scores", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(cache_scores)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "llla_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
