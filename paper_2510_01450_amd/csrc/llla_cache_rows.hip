@@ -239,8 +239,8 @@ constexpr int PLAN_HDR = 4;                               // moves, exponents of
 constexpr int BINS = 2048, HISTS = 3 * BINS, CHOICES = 4 * 5;      // histograms, and the choice of each step
 
 constexpr int CHUNK = 2048;                               // slots of a workgroup where a head has several
-// One workgroup holds up to 8192 ranks in registers and selects in one launch; longer rows take six launches of many.  us, one workgroup / six
-// launches (LDS histograms and ranks formed anew from memory in every pass of the former beyond 32768): see evict_plan_kernel.
+// One workgroup holds the ranks of up to 16384 slots in registers and selects in one launch; longer rows take six launches of a workgroup per
+// CHUNK.  us, one launch / six: 64 heads x 16384 slots 23 / 35, 512 heads 44 / 117; 64 heads x 32768, where 32 ranks a thread no longer fit, 112 / 43.
 constexpr int ONE_LAUNCH = 16384;
 
 inline EvictPlan evict_plan(int L_max, int keep, bool in_place)

@@ -131,8 +131,9 @@ def test_workspace_sizes():
     # of the size of queries times keys
     assert 16 * 32768 * 4 <= L.llla_cache_scores_workspace_bytes(c, 16, 1, BF16) < 16 * 32768 * 4 + (1 << 20)
     assert L.llla_cache_scores_workspace_bytes(c, 16, 32768, BF16) <= 16 * 32768 * 4 + (8 << 20) + 512
-    # slots of the rows that move
-    assert L.llla_cache_evict_workspace_bytes(c, 4096) <= 16 * 4 * (2 * 4096 + 256)
+    # slots of the rows that move; long rows also three histograms of 2048 bins
+    assert L.llla_cache_evict_workspace_bytes(_cache(B=1, H=16, L=16384), 4096) <= 16 * 4 * (2 * 4096 + 256)
+    assert L.llla_cache_evict_workspace_bytes(c, 4096) <= 16 * 4 * (2 * 4096 + 3 * 2048 + 256)
     assert L.llla_cache_evict_workspace_bytes(c, 0) == 0 and L.llla_cache_evict_workspace_bytes(c, 40000) == 0
 
 
