@@ -575,13 +575,17 @@ __device__ __forceinline__ void decode_q8_wide_body(const Q8Args &a, const DecPi
                 for (int J = 0; J < NB; ++J) vraw[J] = read(s, 1, h, J);
             };
             request(0);
-            float t[4];
+            float t[4];                                   // logit of key 32 h + 8 g + 2 (n % 4) + c in t[2 h + c]: a lane's pair is a pair of an operand
+            const int key = 8 * g + 2 * (nn & 3);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int key = 32 * (i / 2) + 8 * g + 4 * (i % 2) + (nn & 3);
-                const f32x4 p = *reinterpret_cast<const f32x4 *>(wl.part[s & 1][key]);
-                t[i] = marked ? NAN : (p[0] + p[1]) + (p[2] + p[3]);
-                t[i] = j0 + key < r1 ? t[i] : -INFINITY;
+                const f32x4 p = *reinterpret_cast<const f32x4 *>(wl.part[s & 1][32 * (i / 2) + key + i % 2]);
+                t[i] = (p[0] + p[1]) + (p[2] + p[3]);
+            }
+            if (marked) t[0] = t[1] = t[2] = t[3] = NAN;  // (scalar branches)
+            if (j0 + KEYS > r1) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t[i] = j0 + 32 * (i / 2) + key + i % 2 < r1 ? t[i] : -INFINITY;
             }
             const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
             if (__builtin_amdgcn_ballot_w64(top > mref + (TOP<TWO> + SLACK)) != 0) {
@@ -595,20 +599,30 @@ __device__ __forceinline__ void decode_q8_wide_body(const Q8Args &a, const DecPi
             }
             mtrue = fmaxf(mtrue, top);
             float w[4];
+            half2q wp[2];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = __builtin_amdgcn_exp2f(t[i] - mref);
-                if constexpr (!TWO) w[i] = (float)(_Float16)w[i];
-                om += w[i];
+            for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(t[i] - mref);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if constexpr (TWO) om += w[2 * h] + w[2 * h + 1];
+                else {
+                    wp[h] = half2q{(_Float16)w[2 * h], (_Float16)w[2 * h + 1]};
+                    om = __builtin_amdgcn_fdot2(wp[h], half2q{(_Float16)1.f, (_Float16)1.f}, om, false);
+                }
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float wc[8] = {row_bcast<0>(w[2 * h]), row_bcast<1>(w[2 * h]), row_bcast<2>(w[2 * h]), row_bcast<3>(w[2 * h]),
-                                     row_bcast<0>(w[2 * h + 1]), row_bcast<1>(w[2 * h + 1]), row_bcast<2>(w[2 * h + 1]), row_bcast<3>(w[2 * h + 1])};
-                half8 x[NR], xl[NR], w8;                  // (xl with two terms, w8 with one)
-                if constexpr (!TWO) {
+                half8 x[NR], xl[NR], w8;                  // the half's weights in the operands' order: w8 with one term, wc (and xl) with two
+                float wc[8];
+                if constexpr (!TWO) w8 = pair_bcast(wp[h]);
+                else {
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) w8[c] = (_Float16)wc[c];
+                    for (int c = 0; c < 2; ++c) {
+                        wc[c] = row_bcast<0>(w[2 * h + c]);
+                        wc[2 + c] = row_bcast<1>(w[2 * h + c]);
+                        wc[4 + c] = row_bcast<2>(w[2 * h + c]);
+                        wc[6 + c] = row_bcast<3>(w[2 * h + c]);
+                    }
                 }
 #pragma unroll
                 for (int i = 0; i < NR; ++i) {
@@ -728,8 +742,7 @@ __device__ __forceinline__ void decode_q8_piece(const Q8Args &a, const DecPiece 
     }
 }
 
-// One term: sequences of at most PRECISE_KEYS are left to precise_heads_kernel.  (Both variants in one kernel spilled, and with spills around its
-// transfers one of them gave wrong moments.)
+// One term: sequences of at most PRECISE_KEYS are left to precise_heads_kernel (one kernel for both has not the registers).
 template <int D> constexpr int PRECISE_KEYS = 4 * D;
 template <int D, typename F, typename TQ, bool FUSED, bool TWO>
 __global__ __launch_bounds__(NT, (D == 128 && FUSED) ? 1 : 2) void decode_q8_kernel(Q8Args a)
