@@ -25,8 +25,9 @@ template <> struct RowType<bf16_t> { static constexpr int SIZE = 2, TERMS = 1; }
 template <> struct RowType<Int8Code> { static constexpr int SIZE = 1, TERMS = 1; };
 template <> struct RowType<E4m3Code> { static constexpr int SIZE = 1, TERMS = 1; };
 
-// Lane (g, n) holds features g D / 4 .. of row n, eight to a step of 32 (at d = 16 four, the others zero): whole rows in loads of up to
-// sixteen bytes.  Any order of the features will do, as long as both operands have it.
+// Lane (g, n) holds a quarter of row n's features, eight to a step of 32 (at d = 16 four, the others zero).  Any order of the features will do, as long as
+// both operands have it: groups of the sixteen bytes of a key go to the four lanes in turn, so that a load reads 64 consecutive bytes of every row (with
+// a lane's bytes consecutive, 128 of an fp32 row at d = 128, lines that were not to be kept were fetched more than once: 14 heads of 4006 rows 27 us).
 template <int D, typename T>
 struct Operand {
     static constexpr int CH = D < 32 ? 1 : D / 32, TERMS = RowType<T>::TERMS;
@@ -40,19 +41,25 @@ struct Words {
     unsigned w[BYTES / 4];
 };
 
-// ONCE: not to be kept in the caches
-template <int D, typename T, bool ONCE = false>
+// features of a group
+template <int D, typename TK> constexpr int GROUP = 16 / RowType<TK>::SIZE < D / 4 ? 16 / RowType<TK>::SIZE : D / 4;
+
+// of a key or, T = TQ, a query to keys of type TK; ONCE: not to be kept in the caches
+template <int D, typename TK, typename T, bool ONCE = false>
 __device__ __forceinline__ Words<D, T> load_words(const char *row, int g)
 {
-    constexpr int BYTES = Words<D, T>::BYTES, N = BYTES < 16 ? BYTES / 4 : 4;
+    constexpr int G = GROUP<D, TK>, BYTES = G * RowType<T>::SIZE, N = BYTES < 16 ? BYTES / 4 : 4, LOADS = BYTES / 4 / N;
     typedef unsigned part __attribute__((ext_vector_type(N)));
     Words<D, T> o;
-    const part *p = reinterpret_cast<const part *>(row + g * BYTES);
 #pragma unroll
-    for (int i = 0; i < BYTES / 4 / N; ++i) {
-        const part v = ONCE ? __builtin_nontemporal_load(p + i) : p[i];
+    for (int i = 0; i < D / 4 / G; ++i) {
+        const part *p = reinterpret_cast<const part *>(row + (4 * i + g) * BYTES);
 #pragma unroll
-        for (int e = 0; e < N; ++e) o.w[N * i + e] = v[e];
+        for (int k = 0; k < LOADS; ++k) {
+            const part v = ONCE ? __builtin_nontemporal_load(p + k) : p[k];
+#pragma unroll
+            for (int e = 0; e < N; ++e) o.w[N * (LOADS * i + k) + e] = v[e];
+        }
     }
     return o;
 }
@@ -220,7 +227,7 @@ constexpr float FAR = 0x1p64f;
 template <int D, typename TK, typename TQ, int RT, bool ROWS>
 __global__ __launch_bounds__(NT, (RegisterFile<D, TK, TQ, RT>::WAVES)) void stats_kernel(ScoresArgs a)
 {
-    constexpr int PF = Words<D, TK>::BYTES > 32 ? 1 : 4;
+    constexpr int PF = Words<D, TK>::BYTES > 64 ? 1 : 4;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16, n = lane % 16;
     const int bh = blockIdx.y;
     const Head x = head_of(a, bh);
@@ -235,7 +242,7 @@ __global__ __launch_bounds__(NT, (RegisterFile<D, TK, TQ, RT>::WAVES)) void stat
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         const Query r(a, r0 + 16 * i + n);
-        query_operand<D, TQ>(q[i], a, load_words<D, TQ>(r.row(a, x), g));
+        query_operand<D, TQ>(q[i], a, load_words<D, TK, TQ>(r.row(a, x), g));
         lim[i] = r.limit(a, x);
         most = max(most, lim[i]);
         least = min(least, r.real ? lim[i] : INT32_MAX);
@@ -245,7 +252,7 @@ __global__ __launch_bounds__(NT, (RegisterFile<D, TK, TQ, RT>::WAVES)) void stat
     const int k1 = min(min(k0 + each, x.len), wave_max(most));
     least = min(wave_min(least), k1);
     const char *Kh = a.K + x.b * a.sk.batch + x.h * a.sk.head;
-    auto load = [&](int j) { return load_words<D, TK, !ROWS && RT == 1>(Kh + (int64_t)min(j + n, x.len - 1) * a.sk.seq, g); };
+    auto load = [&](int j) { return load_words<D, TK, TK, !ROWS && RT == 1>(Kh + (int64_t)min(j + n, x.len - 1) * a.sk.seq, g); };
     if (k0 < k1) {
         Words<D, TK> ahead[PF];
 #pragma unroll
@@ -339,32 +346,32 @@ __global__ __launch_bounds__(NT, (RegisterFile<D, TK, TQ, RT>::WAVES)) void stat
 
 constexpr int FEW = 64;                                   // queries at most that a workgroup's waves share in the statistics
 
-// log2 of the sum of weights of query r, from its parts; by four neighbouring threads
-__device__ __forceinline__ float merged(const ScoresArgs &a, int bh, int r, int sub)
+// log2 of the sum of weights of query r, from its parts; by `width` neighbouring threads (a power of two up to 64)
+__device__ __forceinline__ float merged(const ScoresArgs &a, int bh, int r, int sub, int width)
 {
     float m = -INFINITY, l = 0.f;
     if (r < a.M)
-        for (int s = sub; s < a.splits; s += 4) {
+        for (int s = sub; s < a.splits; s += width) {
             const size_t at = ((size_t)bh * a.splits + s) * a.M + r;
             join(m, l, a.stats[2 * at], a.stats[2 * at + 1]);
         }
-    join(m, l, __shfl_xor(m, 1), __shfl_xor(l, 1));
-    join(m, l, __shfl_xor(m, 2), __shfl_xor(l, 2));
+    for (int off = 1; off < width; off *= 2) join(m, l, __shfl_xor(m, off), __shfl_xor(l, off));
     return l == 0.f ? INFINITY : m + __builtin_amdgcn_logf(l);
 }
 
 // of a head's few queries, in LDS
 __device__ __forceinline__ void merge_few(const ScoresArgs &a, int bh, float (&lse)[FEW])
 {
-    const float v = merged(a, bh, threadIdx.x / 4, threadIdx.x % 4);
-    if (threadIdx.x % 4 == 0) lse[threadIdx.x / 4] = v;
+    const int shift = a.M <= NT / 64 ? 6 : a.M <= NT / 16 ? 4 : 2, r = threadIdx.x >> shift, sub = threadIdx.x & ((1 << shift) - 1);
+    const float v = merged(a, bh, r, sub, 1 << shift);
+    if (sub == 0) lse[r] = v;
     __syncthreads();
 }
 
 __global__ __launch_bounds__(NT) void merge_stats_kernel(ScoresArgs a)
 {
     const int r = blockIdx.x * (NT / 4) + threadIdx.x / 4;
-    const float v = merged(a, blockIdx.y, r, threadIdx.x % 4);
+    const float v = merged(a, blockIdx.y, r, threadIdx.x % 4, 4);
     if (threadIdx.x % 4 == 0 && r < a.M) a.lse[(size_t)blockIdx.y * a.M + r] = v;
 }
 
@@ -411,7 +418,7 @@ __global__ __launch_bounds__(NT, (RegisterFile<D, TK, TQ, 4>::WAVES)) void share
     const char *Kh = a.K + x.b * a.sk.batch + x.h * a.sk.head;
     Operand<D, TK> k[4];
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt) make_operand<D, TK>(k[kt], load_words<D, TK>(Kh + (int64_t)min(j0 + 16 * kt + n, x.len - 1) * a.sk.seq, g));
+    for (int kt = 0; kt < 4; ++kt) make_operand<D, TK>(k[kt], load_words<D, TK, TK>(Kh + (int64_t)min(j0 + 16 * kt + n, x.len - 1) * a.sk.seq, g));
     const float c = tile_scale<TK>(a, bh, j0);
     f32x4 s[4];
 #pragma unroll
@@ -427,7 +434,7 @@ __global__ __launch_bounds__(NT, (RegisterFile<D, TK, TQ, 4>::WAVES)) void share
     auto load = [&](int r0) {
         Tile t;
         const int at = min(r0 + n, a.M - 1);
-        t.q = load_words<D, TQ>(row, g);
+        t.q = load_words<D, TK, TQ>(row, g);
         t.ref = few ? lse[at & (FEW - 1)] : a.lse[(size_t)bh * a.M + at];
         t.lim = r.limit(a, x);
         r.i += rest;
@@ -488,9 +495,10 @@ ScoresPlan scores_plan(const llla_cache &c, int H, int nq, llla_dtype in)
     p.M = H / c.H * nq;
     const int heads = c.B * c.H, size = c.type == LLLA_F32 ? 4 : c.type == LLLA_BF16 ? 2 : 1;
     if (p.M <= FEW) {
-        // six workgroups per compute unit, all resident (512 heads of 32768 int8 keys: 255 us; four 258, eight, in two turns, 272, and more
-        // leave more parts to merge: 263 with sixteen), each wave with at least 256 keys
-        const int wgs = std::max(1, std::min((1536 + heads - 1) / heads, (c.L_max + 1023) / 1024));
+        // Six workgroups per compute unit, all resident (512 heads of 32768 int8 keys: 255 us; four 258, eight, in two turns, 272), of at least 1024
+        // keys, or 256 while there are fewer than two per compute unit (14 heads of 4006 fp32 rows at d = 128 23 -> 13 us, 16 of 4096 int8
+        // rows 8.1 -> 6.4): more parts cost their merging.
+        const int wgs = std::max({1, std::min((1536 + heads - 1) / heads, (c.L_max + 1023) / 1024), std::min(512 / heads, (c.L_max + 255) / 256)});
         p.splits = NW * wgs;
         // a logit is written and read, a row of the cache would be read a second time
         p.stored = 8 * p.M <= c.d * size;
