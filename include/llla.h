@@ -292,9 +292,11 @@ llla_status llla_cache_append(const llla_cache *cache, const void *k, const void
  *   q       : device, [B, H, d] contiguous, dtype `in` (LLLA_F32 or LLLA_BF16);  H a multiple of cache->H
  *   o       : device, [B, H, d] contiguous, dtype `out`
  *   seqlens : valid lengths, or NULL = all L_max; the result of an empty sequence is zero
- * fp32 arithmetic for every type: sequences of at most 64 keys in key space in fp64, longer ones on 16-bit matrix instructions that take
- * the codes as they are and the weighted keys in two terms of 11 bits.  There is no range of values to keep to; rows of a block whose exponent is
- * more than 15 (int8) or 22 (e4m3) below the largest of their head's lose low bits, at most 2^-23 of the largest row.
+ * Sequences of at most 64 keys are solved in key space in fp64; longer ones on 16-bit matrix instructions, which take the codes as they are, sums
+ * in fp32.  Weighted keys have two terms of 11 bits (the precision of fp32) where the result is fp32 or the sequence has at most 4 d keys, otherwise
+ * one: 2.5e-4 of the result, a seventh of a bf16 result's rounding.  There is no range of values to keep to.  Keys and values are taken relative to the largest
+ * exponent among blocks that are read together: blocks more than 15 (int8) or 4 (e4m3) exponents below it lose low bits, at most 2^-21 of the
+ * largest key or value there.
  * Workspace: llla_decode_q8_workspace_bytes, or NULL (or less): one workgroup per head, slow for long caches of few heads.
  */
 size_t llla_decode_q8_workspace_bytes(const llla_cache *cache, int H);

@@ -110,7 +110,8 @@ struct AppendArgs {
 };
 
 // One workgroup per block of 64 slots that new rows may fall into: it sees all new rows of its block, so the exponent, and the codes with it, are
-// written once, and no two workgroups touch a block.  Traffic is what bounds it: every value is read once and written once.
+// written once, and no two workgroups touch a block.  Traffic is what bounds it: every value is read once and written once (128 heads x 1535 bf16 rows
+// of 64 to int8 17 us, 4.4 TB/s read and written; one token of 512 heads 5 us, its launch).
 template <int D, typename TI, typename C>
 __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a)
 {
@@ -689,7 +690,8 @@ __device__ __forceinline__ void move_row_words(const MoveArgs &a, int bh, int fr
     if (a.index) a.index[(size_t)bh * a.keep + to] = from;
 }
 
-// Rows of numbers: copies, MOVE_ROWS of a head per workgroup, sixteen bytes per thread at a time
+// Rows of numbers: copies, MOVE_ROWS of a head per workgroup, sixteen bytes per thread at a time (64 heads x 4096 rows of 256 bytes, keys and values:
+// 63 us, 4.3 TB/s read and written)
 constexpr int MOVE_ROWS = 32;
 template <int ROW_BYTES>
 __global__ __launch_bounds__(NT) void move_kernel(MoveArgs a)
@@ -794,7 +796,7 @@ __global__ __launch_bounds__(NT) void move_codes_kernel(MoveArgs a)
     }
 }
 
-// Rows of codes in place: one wave per block of destinations, most of which have few holes or none.  In these moments the block that holds slot
+// Rows of codes in place: one wave per block of destinations, most of which have few holes or none (256 heads x 64 rows into 4096 slots 10 us).  In these moments the block that holds slot
 // `keep` may be getting another exponent; rows that come from it take the one that the plan saw.
 template <int D, typename F>
 __global__ __launch_bounds__(NT) void fill_holes_kernel(MoveArgs a)

@@ -5,7 +5,9 @@
 // are sums in a lane with one exchange at the end.  Two passes, because a share needs its query's omega: statistics (largest logit and sum of
 // weights per query), then shares.  Codes and bf16 numbers are operands as they are; fp32 is split into three bf16 (24 bits), six products.
 //   few queries (decode): the first pass is bound by the cache's traffic; it leaves the logits, and the second reads those
-//   many (prompts): both passes form the logits; what bounds them is one exponential per logit and pass
+//     (512 heads x 32768 int8 keys 220 + 32 us, 4.9 TB/s)
+//   many (prompts): both passes form the logits; per logit and pass one exponential, one multiply-add and one addition on the vector port
+//     (32 heads, 4096 queries over 4096 bf16 keys: 124 + 116 us, 2.2 logits per ns and pass; vector port 40-50 %, the rest waits for rows)
 #include <algorithm>
 
 #include "llla_cache.hpp"

@@ -75,7 +75,9 @@ def test_lengths_of_their_own(dtype, d, group):
     seq = torch.tensor(lens, dtype=torch.int32, device=DEV)
     got = llla.llla_decode_q8(q, cache, LAM, 1 / math.sqrt(d), seqlens=seq)
     _check(got, q, cache, 1 / math.sqrt(d), lens, "d=%d group=%d" % (d, group))
-    # (a bf16 result: two terms up to 4 d keys, one beyond; 11 bits of x lose 2^-12 |z| / sqrt(lambda w) .. of badly conditioned heads: see the unit keys above)
+    # A bf16 result of more than 4 d keys has one term: x = w k is off by 2^-11 of itself, a moment by at most 2^-11 of the sum of w |k| |k|'.  The solve passes
+    # that on by one over the smallest eigenvalue of Sigma / omega, (1 - sqrt(d / n))^2 of the keys' variance, 1/3 at d = 128 and 700 keys: 3 x 2^-11, up to
+    # 2^-9.  It comes in from mu, Sigma and the value moments, and weights that differ leave fewer keys than n: 2^-7 in all.
     got = llla.llla_decode_q8(q, cache, LAM, 1 / math.sqrt(d), seqlens=seq, out_dtype=BF16)
     assert got.dtype == BF16
     _check(got, q, cache, 1 / math.sqrt(d), lens, "d=%d group=%d bf16" % (d, group), far=2.0 ** -7)
