@@ -64,7 +64,7 @@ typedef enum {
     LLLA_ERR_NULL = 1,        /* a required pointer is NULL */
     LLLA_ERR_SHAPE = 2,       /* B, H, n, L or d <= 0, or a stride too small for the shape */
     LLLA_ERR_DTYPE = 3,       /* unknown llla_dtype */
-    LLLA_ERR_PARAM = 4,       /* lambda <= 0 or not finite, scale not finite */
+    LLLA_ERR_PARAM = 4,       /* lambda <= 0 or not finite, scale not finite; rows kept or protected out of range, one array given twice */
     LLLA_ERR_ALIGN = 5,       /* base pointer or stride not 16-byte compatible */
     LLLA_ERR_WORKSPACE = 6,   /* workspace NULL/unaligned or smaller than *_workspace_bytes() */
     LLLA_ERR_UNSUPPORTED = 7, /* d not in {16, 32, 64, 128}, or a path forced that does not serve the call */
@@ -248,7 +248,7 @@ llla_status llla_decode_static(const void *q, const void *Kc, const void *Vc, vo
  * The cache of a serving loop, and what is done to it between two tokens: rows are stored, attended to, weighed and given up.
  *
  * llla_cache -- keys and values of B sequences and H cache heads, slots 0 .. L_max - 1.
- *   K, V         : device, [B, H, L_max, d] in `type`, strides sk / sv (8-bit types: multiples of 16 elements; below 2^27)
+ *   K, V         : device, [B, H, L_max, d] in `type`, strides sk / sv (8-bit types: multiples of 16 elements; of rows below 2^25); L_max <= 2^30, B * H <= 65535
  *   k_exp, v_exp : device int8 [B, H, ceil(L_max / LLLA_CACHE_BLOCK)] contiguous; 8-bit types only, ignored otherwise
  *   scores       : device float [B, H, L_max] contiguous: the weight a row has gathered; NULL where a call does not need it
  *   pos          : device int32 [B, H, L_max] contiguous: the position in its sequence that a row stands for; NULL: its slot
@@ -259,7 +259,7 @@ llla_status llla_decode_static(const void *q, const void *Kc, const void *Vc, vo
  * The exponent of a block is the smallest e >= -120 with max |x| <= 127 * 2^e (int8) or 448 * 2^e (e4m3), rows are rounded to the nearest code,
  * ties to even.  It only grows while rows come in, in which case the rows that are there are rounded again: in e4m3 exactly, but for subnormal codes.
  * Lengths (seqlens: device int32 [B]) are taken as 0 .. L_max; slots at and behind a sequence's length hold nothing, and are written by
- * llla_cache_append alone.  Calls that write a cache and others that use it are ordered by the caller, on one stream or by events.
+ * llla_cache_append alone.  In a cache that is written K and V, and their exponents, are two arrays.  Calls that write a cache and others that use it are ordered by the caller, on one stream or by events.
  */
 #define LLLA_CACHE_BLOCK 64
 

@@ -323,7 +323,7 @@ const char *llla_status_string(llla_status s)
         case LLLA_ERR_NULL: return "a required pointer is NULL";
         case LLLA_ERR_SHAPE: return "bad shape or stride";
         case LLLA_ERR_DTYPE: return "unknown dtype";
-        case LLLA_ERR_PARAM: return "lambda must be finite and > 0, scale finite, path valid, rows kept and protected in range";
+        case LLLA_ERR_PARAM: return "lambda must be finite and > 0, scale finite, path valid, rows kept and protected in range, no array given twice";
         case LLLA_ERR_ALIGN: return "pointers and strides must keep rows 16-byte aligned";
         case LLLA_ERR_WORKSPACE: return "workspace missing, unaligned or too small";
         case LLLA_ERR_UNSUPPORTED: return "unsupported head dimension or path";

@@ -22,7 +22,7 @@ bool strides_aligned(const llla_strides &s, llla_dtype t)
     return s.batch % q == 0 && s.head % q == 0 && s.seq % q == 0;
 }
 
-constexpr int64_t MAX_ROW_STRIDE = (int64_t)1 << 27;      // elements: offsets of a few rows are kept in 32 bits
+constexpr int64_t MAX_ROW_STRIDE = (int64_t)1 << 25;      // elements: offsets of 64 rows are kept in 32 bits
 
 // values: whether V is used
 llla_status check_cache(const llla_cache *c, bool values)
@@ -40,6 +40,9 @@ llla_status check_cache(const llla_cache *c, bool values)
         return LLLA_ERR_ALIGN;
     return LLLA_OK;
 }
+
+// keys and values of a cache that is written must be two arrays
+bool twice(const llla_cache &c) { return c.K == c.V || (codes(c.type) && c.k_exp == c.v_exp); }
 
 llla_status check_workspace(size_t need, const void *ws, size_t bytes)
 {
@@ -60,6 +63,7 @@ llla_status llla_cache_append(const llla_cache *cache, const void *k, const void
     if (st != LLLA_OK) return st;
     if (n <= 0) return LLLA_ERR_SHAPE;
     if (!number_type(in)) return LLLA_ERR_DTYPE;
+    if (twice(*cache)) return LLLA_ERR_PARAM;
     if (!strides_cover(sk, cache->B, cache->H, n, cache->d) || !strides_cover(sv, cache->B, cache->H, n, cache->d)) return LLLA_ERR_SHAPE;
     if (!aligned(k, 16) || !aligned(v, 16) || !strides_aligned(sk, in) || !strides_aligned(sv, in) || !aligned(seqlens, 4) ||
         !aligned(new_lens, 4) || !aligned(first_pos, 4))
@@ -129,13 +133,13 @@ llla_status llla_cache_evict(const llla_cache *cache, const llla_cache *into, co
     if (st != LLLA_OK) return st;
     if (!cache->scores || !lens) return LLLA_ERR_NULL;
     if (keep <= 0 || keep > cache->L_max) return LLLA_ERR_SHAPE;
-    if (sinks < 0 || recent < 0 || (int64_t)sinks + recent > keep || lens == seqlens) return LLLA_ERR_PARAM;
+    if (sinks < 0 || recent < 0 || (int64_t)sinks + recent > keep || lens == seqlens || (!into && twice(*cache))) return LLLA_ERR_PARAM;
     if (into) {
         st = check_cache(into, true);
         if (st != LLLA_OK) return st;
         if (into->B != cache->B || into->H != cache->H || into->d != cache->d || into->L_max < keep) return LLLA_ERR_SHAPE;
         if (into->type != cache->type) return LLLA_ERR_DTYPE;
-        if (into->K == cache->K || into->V == cache->V || into->K == into->V || (into->scores && into->scores == cache->scores) ||
+        if (into->K == cache->K || into->V == cache->V || into->K == cache->V || into->V == cache->K || twice(*into) || (into->scores && into->scores == cache->scores) ||
             (into->pos && into->pos == cache->pos) || (codes(cache->type) && (into->k_exp == cache->k_exp || into->v_exp == cache->v_exp)))
             return LLLA_ERR_PARAM;
     }

@@ -41,6 +41,7 @@ BAD_CACHES = [
     (dict(K=0), 1), (dict(V=0), 1), (dict(k_exp=0), 1), (dict(v_exp=0), 1),
     (dict(B=0), 2), (dict(L=0), 2), (dict(d=-1), 2), (dict(B=70000), 2), (dict(sk=_Strides(0, 64 * 128, 64)), 2), (dict(sv=_Strides(16384, 0, 64)), 2),
     (dict(sk=_Strides(16384, 8192, 48)), 2), (dict(sk=_Strides(1 << 40, 1 << 34, 1 << 27)), 2), (dict(sv=_Strides(16384, 8192, -64)), 2),
+    (dict(sk=_Strides(1 << 40, 1 << 34, 1 << 25)), 2), (dict(L=(1 << 30) + 64), 2),
     (dict(type=4), 3), (dict(type=-1), 3),
     (dict(K=FAKE + 8), 5), (dict(V=FAKE + 1), 5), (dict(sk=_Strides(16384, 8192, 72)), 5), (dict(scores=FAKE + 2), 5), (dict(pos=FAKE + 1), 5),
     (dict(d=48), 7), (dict(d=256), 7),
@@ -69,6 +70,14 @@ def test_missing_cache():
 ])
 def test_append_refuses(kw, code):
     assert _append(_cache(), **kw) == code
+
+
+def test_keys_and_values_in_one_array():
+    """Read, they may be one; written, they would be written twice."""
+    for kw in (dict(V=FAKE), dict(v_exp=3 * FAKE)):
+        assert _append(_cache(**kw)) == 4 and _evict(_cache(**kw)) == 4
+        assert _evict(_cache(), into=_cache(**dict(dict(K=7 * FAKE, V=8 * FAKE, k_exp=9 * FAKE, v_exp=10 * FAKE, scores=0, pos=0), **{k: 7 * FAKE if k == "V" else 9 * FAKE for k in kw}))) == 4
+        assert _scores(_cache(**kw)) == 6
 
 
 @pytest.mark.parametrize("kw,code", [
