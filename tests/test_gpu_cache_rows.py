@@ -301,3 +301,16 @@ def test_last_bits_of_a_very_long_cache():
     # slots 0 .. 99 have score 0: the last of them are given up
     assert torch.equal(cache.K[0, :, 100 - n:100], k[0]) and torch.equal(cache.V[0, :, 100 - n:100], v[0])
     assert not cache.K[0, :, :100 - n].any() and torch.equal(cache.scores[0, :, 100 - n:100], torch.full((H, n), 5.0, device=DEV))
+
+
+@pytest.mark.parametrize("dtype", [I8, BF16])
+@pytest.mark.parametrize("into", [False, True])
+def test_evicted_rows_far_apart(dtype, into):
+    """Rows 16 MB and more apart, 4.4 GB and more in all: as with rows together."""
+    L, d, pitch = 260, 32, 17 << 20
+    gen = _gen(71)
+    cache = _cache(gen, 1, 2, L, d, dtype, [L])
+    flat = torch.zeros((L - 1) * pitch + 2 * d, dtype=dtype, device=DEV)
+    K = flat.as_strided((1, 2, L, d), (0, d, pitch, 1))
+    K.copy_(cache.K)
+    _evict(cache._replace(K=K), [L], 133, sinks=3, recent=20, into=_cache(gen, 1, 2, 140, d, dtype, [0]) if into else None)

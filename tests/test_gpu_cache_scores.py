@@ -149,3 +149,16 @@ def test_strides_and_stream():
     llla.llla_cache_scores(Qt, cache._replace(K=K), 0.125, stream=s)
     torch.cuda.current_stream().wait_stream(s)
     assert torch.equal(cache.scores, want)
+
+
+@pytest.mark.parametrize("nq", [1, 80])
+def test_offsets_beyond_32_bits(nq):
+    """Rows 4 MB apart, 2.5 GB in all: the same bits as with rows together."""
+    cache, Q = _case(1, 2, 2, 620, 64, I8, nq, BF16, 11)
+    before = cache.scores.clone()
+    want = llla.llla_cache_scores(Q, cache, 0.125).clone()
+    cache.scores.copy_(before)
+    flat = torch.zeros(620 * (4 << 20) + 128, dtype=I8, device=DEV)
+    K = flat.as_strided((1, 2, 620, 64), (0, 64, 4 << 20, 1))
+    K.copy_(cache.K)
+    assert torch.equal(llla.llla_cache_scores(Q, cache._replace(K=K), 0.125), want)

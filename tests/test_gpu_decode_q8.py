@@ -246,3 +246,18 @@ def test_offsets_beyond_32_bits():
     V = flat.as_strided((1, HC, L, d), (0, d, pitch, 1))
     V.copy_(cache.V)
     assert torch.equal(llla.llla_decode_q8(q, cache._replace(V=V), LAM, 0.125), want)
+
+
+@pytest.mark.parametrize("d", [16, 32])
+@pytest.mark.parametrize("L", [90, 140])
+def test_rows_as_far_apart_as_they_may_be(d, L):
+    """The largest row stride; lengths that end inside a block (rows of a transfer are read from 32-bit offsets)."""
+    pitch = (1 << 25) - 16
+    q, cache = _case(1, 2, 2, L, d, E4M3, BF16, L + d, unit=True)
+    want = llla.llla_decode_q8(q, cache, LAM, 0.25)
+    flat = torch.zeros((L - 1) * pitch + 2 * d, dtype=torch.uint8, device=DEV).view(E4M3)
+    K = flat.as_strided((1, 2, L, d), (0, d, pitch, 1))
+    K.copy_(cache.K)
+    assert torch.equal(llla.llla_decode_q8(q, cache._replace(K=K), LAM, 0.25), want)
+    one = llla.llla_decode_q8(q, cache, LAM, 0.25, out_dtype=BF16)
+    assert torch.equal(llla.llla_decode_q8(q, cache._replace(K=K), LAM, 0.25, out_dtype=BF16), one)
