@@ -7,7 +7,8 @@
 //   few queries (decode): the first pass is bound by the cache's traffic; it leaves the logits, and the second reads those
 //     (512 heads x 32768 int8 keys 220 + 32 us, 4.9 TB/s)
 //   many (prompts): both passes form the logits; per logit and pass one exponential, one multiply-add and one addition on the vector port
-//     (32 heads, 4096 queries over 4096 bf16 keys: 124 + 116 us, 2.2 logits per ns and pass; vector port 40-50 %, the rest waits for rows)
+//     (32 heads, 4096 queries over 4096 bf16 keys: 82 + 88 us, 3.2 logits per ps and pass; the least that those three instructions take, 17
+//     cycles of a wave as measured, is 29 us a pass; rows come from L2)
 #include <algorithm>
 
 #include "llla_cache.hpp"
@@ -527,10 +528,11 @@ ScoresPlan scores_plan(const llla_cache &c, int H, int nq, llla_dtype in)
     } else {
         const int rows = 16 * (in == LLLA_F32 ? 2 : 4) * NW;
         p.blocks = (p.M + rows - 1) / rows;
-        // parts of the keys, for sixteen workgroups per compute unit (queries of a prompt see few keys or many, and four are resident), but
-        // of at least 512 keys, or 128 while there are fewer workgroups than compute units
+        // parts of the keys, for four workgroups per compute unit (queries of a prompt see few keys or many, and two are resident: 155 us for 32 heads
+        // of 4096 bf16 keys and queries; sixteen, which begin and end more often, 174, two 167), but of at least 512 keys, or 128 while there are
+        // fewer workgroups than twice the compute units
         const int64_t each = (int64_t)heads * p.blocks;
-        p.splits = (int)std::max<int64_t>({1, std::min<int64_t>(4096 / each, (c.L_max + 511) / 512), std::min<int64_t>(512 / each, (c.L_max + 127) / 128)});
+        p.splits = (int)std::max<int64_t>({1, std::min<int64_t>(1024 / each, (c.L_max + 511) / 512), std::min<int64_t>(512 / each, (c.L_max + 127) / 128)});
     }
     p.pitch = p.stored ? (int64_t)(c.L_max + 63) / 64 * 64 : 0;
     p.stats_bytes = p.blocks && p.splits == 1 ? 0 : round_up((size_t)heads * p.M * 2 * p.splits * sizeof(float), 256);

@@ -136,7 +136,7 @@ def test_workspace_sizes():
     L = llla.lib()
     c = _cache(B=1, H=16, L=32768)
     assert L.llla_decode_q8_workspace_bytes(c, 16) > 0 and L.llla_decode_q8_workspace_bytes(_cache(L=64), 4) == 0
-    # decode steps keep their logits; prompts one number per query, and two per query and part of the keys, 4096 parts of 256 queries at most (8 MiB): nothing
+    # decode steps keep their logits; prompts one number per query, and two per query and part of the keys, never more than 4096 parts of 256 queries (8 MiB): nothing
     # of the size of queries times keys
     assert 16 * 32768 * 4 <= L.llla_cache_scores_workspace_bytes(c, 16, 1, BF16) < 16 * 32768 * 4 + (1 << 20)
     assert L.llla_cache_scores_workspace_bytes(c, 16, 32768, BF16) <= 16 * 32768 * 4 + (8 << 20) + 512
