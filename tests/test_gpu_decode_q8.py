@@ -261,3 +261,16 @@ def test_rows_as_far_apart_as_they_may_be(d, L):
     assert torch.equal(llla.llla_decode_q8(q, cache._replace(K=K), LAM, 0.25), want)
     one = llla.llla_decode_q8(q, cache, LAM, 0.25, out_dtype=BF16)
     assert torch.equal(llla.llla_decode_q8(q, cache._replace(K=K), LAM, 0.25, out_dtype=BF16), one)
+
+
+@pytest.mark.parametrize("d", [16, 64, 128])
+@pytest.mark.parametrize("out", [F32, BF16])
+def test_without_a_workspace(d, out):
+    """A workspace that is too small is none: one workgroup per head, every kind of length; and the others behind the result stay as they were."""
+    lens = [0, 1, 64, 65, 4 * d, 4 * d + 1, 1500]
+    q, cache = _case(7, 4, 2, 1500, d, E4M3, BF16, d, spread=0.1)
+    seq = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    room = torch.full((9, 4, d), 7.0, dtype=out, device=DEV)
+    got = llla.llla_decode_q8(q, cache, LAM, 1 / math.sqrt(d), seqlens=seq, out=room[1:8], workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+    _check(got, q, cache, 1 / math.sqrt(d), lens, "no workspace d=%d %s" % (d, "bf16" if out == BF16 else "f32"), far=2.0 ** -7 if out == BF16 else 0.0)
+    assert bool((room[0] == 7).all()) and bool((room[8] == 7).all())
